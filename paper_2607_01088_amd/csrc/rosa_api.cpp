@@ -15,6 +15,7 @@
 #include "../../include/rosa.h"
 #include "../../include/rosa_debug.h"
 #include "rosa_internal.h"
+#include "rosa_plan.h"
 
 using namespace rosa;
 
@@ -229,47 +230,6 @@ const char *kClassNames[kcCount] = {"time_conditioning", "setup_rows", "in_proj"
 
 thread_local std::string g_create_error;
 
-struct Plan {
-  std::vector<int32_t> order;        // plan position -> caller index
-  std::vector<int32_t> tok_off;      // by plan position
-  std::vector<int32_t> steps;        // by plan position: Euler steps this call runs
-  std::vector<int32_t> m_k;          // per step
-  std::vector<int32_t> n_active;     // per step
-  std::vector<float> taus;
-  std::vector<int32_t> tau_idx;      // [max_K][n]
-  // Attention work: set 0 serves joint (or, alternating, cross-attention)
-  // layers, set 1 the self-attention layers of the alternating layout.  The
-  // device holds set 0's items then set 1's (likewise groups); launch orders
-  // index the whole item array; partial slots are numbered across both sets.
-  struct AttnSet {
-    std::vector<AttnItem> items;
-    std::vector<AttnGroup> groups;
-    std::vector<int32_t> items_upto;   // items of plan requests [0, r]
-    std::vector<int32_t> groups_upto;
-    int item_base = 0, group_base = 0;
-  };
-  AttnSet sets[2];
-  int n_sets = 1;
-  int slots = 0;
-  int M0 = 0, Kmax = 0;
-  // Lanes: disjoint request sets run as independent sub-batches on their own
-  // streams.  Lane l owns plan positions [req_lo, req_hi) and stacked rows
-  // [row_lo, row_hi); at step k its active requests and rows are the prefixes
-  // n_act[k] and m[k] of those ranges (each lane is sorted by K descending).
-  struct Lane {
-    int req_lo = 0, req_hi = 0, row_lo = 0, row_hi = 0;
-    std::vector<int32_t> n_act, m;
-    // Per attention set and step: offset of the attention launch order in
-    // attn_lists, and the launch's block count.
-    std::vector<int32_t> list_at[2], list_blocks[2];
-  };
-  std::vector<Lane> lanes;
-  // Attention launch orders, one per distinct set of active requests of a
-  // lane: the persistent blocks' item lists (item index per entry, -1: an
-  // idle block) and each entry's link to its block's next entry.
-  std::vector<int32_t> attn_lists, attn_next;
-};
-
 }  // namespace
 
 struct rosa_batch {
@@ -355,6 +315,15 @@ rosa_status device_fail(rosa_batch *b, hipError_t e, const char *what) {
   return ROSA_E_DEVICE;
 }
 
+// Query blocks of R query rows: 32-row groups, at most `per` per block (4 per
+// wave group of the bf16 kernel; the fp32 kernel takes any block).
+int attn_query_blocks(int R, int per) { return ((R + 31) / 32 + per - 1) / per; }
+int attn_groups_per_block(const rosa_model_config *cfg) { return 4 * attn_groups_per_wave(cfg->head_dim); }
+
+}  // namespace
+
+namespace rosa {
+
 rosa_status check_config(const rosa_model_config *c) {
   if (c->n_layers < 1 || c->d_model < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->head_dim < 1 ||
       c->d_mlp < 1 || c->action_dim < 1 || c->time_emb_dim < 2 || !(c->rms_eps >= 0.f))
@@ -389,21 +358,13 @@ Dims make_dims(const rosa_model_config *c) {
   return d;
 }
 
-// Query blocks of R query rows: 32-row groups, at most `per` per block (4 per
-// wave group of the bf16 kernel; the fp32 kernel takes any block).
-int attn_query_blocks(int R, int per) { return ((R + 31) / 32 + per - 1) / per; }
-int attn_groups_per_block(const rosa_model_config *cfg) { return 4 * attn_groups_per_wave(cfg->head_dim); }
-
-// Attention set of a layer: 0 for joint layers and the alternating layout's
-// cross-attention (even) layers, 1 for its self-attention (odd) layers.
 int attn_set_of(const rosa_model_config *cfg, int layer) {
   return cfg->attention_layout == ROSA_ATTN_ALTERNATING && (layer & 1) ? 1 : 0;
 }
 
-// Validation of a request set (all-or-nothing) and the batch plan.
 rosa_status build_plan(const rosa_model_config *cfg, const rosa_capacity *cap, const rosa_request *reqs,
                        int n, bool sort_by_steps, bool allow_split, int lanes_wanted, Plan &p, std::string &err,
-                       int max_steps_call = INT32_MAX, int max_slots = -1) {
+                       int max_steps_call, int max_slots) {
   if (n < 0) { err = "n_reqs < 0"; return ROSA_E_INVALID; }
   if (n > 0 && !reqs) { err = "reqs is NULL"; return ROSA_E_INVALID; }
   if (n > cap->max_requests) { err = "more requests than max_requests"; return ROSA_E_CAPACITY; }
@@ -612,6 +573,10 @@ rosa_status build_plan(const rosa_model_config *cfg, const rosa_capacity *cap, c
     }
   return ROSA_OK;
 }
+
+}  // namespace rosa
+
+namespace {
 
 template <typename T>
 T *dalloc(rosa_batch *b, size_t count, hipError_t &e) {
