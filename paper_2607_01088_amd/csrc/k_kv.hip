@@ -1,0 +1,469 @@
+// Operators on prefix caches: conversion to and from 4 bits, eviction of
+// tokens, and plain forms of the attention over either format and of the
+// attention weight that cached tokens gather.
+#include <math.h>
+
+#include <algorithm>
+
+#include "rosa_device.h"
+#include "rosa_internal.h"
+
+namespace rosa {
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+// ------------------------------------------------------------------ to 4 bits and back
+// A block of 32 elements x: a = max |x|, e = the least integer with
+// a <= 7 2^e (a normal a = 1.m 2^E: E - 2 where 1.m <= 1.75, else E - 1),
+// code = x / 2^e rounded to the nearest of {0, .5, 1, 1.5, 2, 3, 4, 6} (ties to the
+// even code).  7 2^e and not 6 2^e: magnitudes in (6, 7] round to 6 anyway,
+// and of the borders between 6 and 8 (every one there is) 7 gives normal
+// data the least error (relative 0.1119; 6: 0.1154, 8: 0.1150).
+//
+// A thread takes 8 elements (16 or 32 bytes in, 4 bytes of codes out, both
+// contiguous over a wave), four threads a block.
+template <typename T>
+__global__ void __launch_bounds__(256) kv_quantize_kernel(KvJobs jobs, int L, int nkv, int hd) {
+  const KvJob &j = jobs.j[blockIdx.y];
+  const T *src = reinterpret_cast<const T *>(blockIdx.z ? j.sv : j.sk);
+  uint8_t *dst = reinterpret_cast<uint8_t *>(blockIdx.z ? j.dv : j.dk);
+  const size_t n8 = (size_t)L * j.P * nkv * (hd / 8);     // a multiple of 4: a block's threads end together
+  uint8_t *scales = dst + kv4_code_bytes(L, j.P, nkv, hd);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
+    uint32_t x[8];                                        // fp32 bits
+    if constexpr (sizeof(T) == 2) {
+      const uint4 w = reinterpret_cast<const uint4 *>(src)[i];
+      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { x[2 * q] = ww[q] << 16; x[2 * q + 1] = ww[q] & 0xffff0000u; }
+    } else {
+      const uint4 w0 = reinterpret_cast<const uint4 *>(src)[2 * i], w1 = reinterpret_cast<const uint4 *>(src)[2 * i + 1];
+      x[0] = w0.x; x[1] = w0.y; x[2] = w0.z; x[3] = w0.w; x[4] = w1.x; x[5] = w1.y; x[6] = w1.z; x[7] = w1.w;
+    }
+    uint32_t a = 0;                                       // magnitudes order as their bits, NaN above all
+#pragma unroll
+    for (int q = 0; q < 8; ++q) a = max(a, x[q] & 0x7fffffffu);
+    a = max(a, (uint32_t)__shfl_xor((int)a, 1, 64));
+    a = max(a, (uint32_t)__shfl_xor((int)a, 2, 64));
+    const bool finite = a < 0x7f800000u;
+    const int E = (int)(a >> 23) - 127;
+    const int e = min(125, max(-125, (a & 0x7fffffu) <= 0x600000u ? E - 2 : E - 1));
+    const float scale = __uint_as_float((uint32_t)(e + 127) << 23);
+    uint32_t c = 0;
+    if (finite) {
+      // the conversion divides by the scale, rounds half to even and saturates
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(x[0]), __uint_as_float(x[1]), scale, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(x[2]), __uint_as_float(x[3]), scale, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(x[4]), __uint_as_float(x[5]), scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(x[6]), __uint_as_float(x[7]), scale, 3);
+    }
+    reinterpret_cast<uint32_t *>(dst)[i] = c;
+    if ((threadIdx.x & 3) == 0) scales[i >> 2] = finite ? (uint8_t)(e + 127) : 255;
+  }
+}
+
+// A scale byte as the fp32 factor the conversions take; byte 255 turns every code to NaN.
+__device__ __forceinline__ float kv4_scale(uint8_t b) { return __uint_as_float((uint32_t)b << 23); }
+
+// 8 codes (4 bytes) as 8 bf16 values.
+__device__ __forceinline__ bf16x8 kv4_bf16x8(uint32_t c, float scale) {
+  const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0);
+  const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+  const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2);
+  const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+  return __builtin_bit_cast(bf16x8, make_uint4(__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1),
+                                               __builtin_bit_cast(uint32_t, v2), __builtin_bit_cast(uint32_t, v3)));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) kv_expand_kernel(KvJobs jobs, int L, int nkv, int hd) {
+  const KvJob &j = jobs.j[blockIdx.y];
+  const uint8_t *src = reinterpret_cast<const uint8_t *>(blockIdx.z ? j.sv : j.sk);
+  T *dst = reinterpret_cast<T *>(blockIdx.z ? j.dv : j.dk);
+  const size_t n8 = (size_t)L * j.P * nkv * (hd / 8);
+  const uint8_t *scales = src + kv4_code_bytes(L, j.P, nkv, hd);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
+    const bf16x8 v = kv4_bf16x8(reinterpret_cast<const uint32_t *>(src)[i], kv4_scale(scales[i >> 2]));
+    if constexpr (sizeof(T) == 2) {
+      reinterpret_cast<uint4 *>(dst)[i] = __builtin_bit_cast(uint4, v);
+    } else {
+      float4 f0 = make_float4((float)v[0], (float)v[1], (float)v[2], (float)v[3]);
+      float4 f1 = make_float4((float)v[4], (float)v[5], (float)v[6], (float)v[7]);
+      reinterpret_cast<float4 *>(dst)[2 * i] = f0;
+      reinterpret_cast<float4 *>(dst)[2 * i + 1] = f1;
+    }
+  }
+}
+
+// Blocks of 256 threads along x for the largest of the jobs' unit counts.
+static int grid_x(size_t most_units, int most_blocks) {
+  return (int)std::min<size_t>((most_units + 255) / 256, (size_t)most_blocks);
+}
+
+static size_t most_units8(const KvJobs &jobs, int n, int L, int nkv, int hd) {
+  int P = 0;
+  for (int i = 0; i < n; ++i) P = std::max(P, jobs.j[i].P);
+  return (size_t)L * P * nkv * (hd / 8);
+}
+
+hipError_t launch_kv_quantize(const KvJobs &jobs, int n, int L, int nkv, int hd, bool bf16_mode, hipStream_t s) {
+  const size_t u = most_units8(jobs, n, L, nkv, hd);
+  if (n <= 0 || u == 0) return hipSuccess;
+  dim3 grid(grid_x(u, 4096), n, 2);
+  if (bf16_mode) hipLaunchKernelGGL(kv_quantize_kernel<bf16>, grid, dim3(256), 0, s, jobs, L, nkv, hd);
+  else hipLaunchKernelGGL(kv_quantize_kernel<float>, grid, dim3(256), 0, s, jobs, L, nkv, hd);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_expand(const KvJobs &jobs, int n, int L, int nkv, int hd, bool bf16_mode, hipStream_t s) {
+  const size_t u = most_units8(jobs, n, L, nkv, hd);
+  if (n <= 0 || u == 0) return hipSuccess;
+  dim3 grid(grid_x(u, 4096), n, 2);
+  if (bf16_mode) hipLaunchKernelGGL(kv_expand_kernel<bf16>, grid, dim3(256), 0, s, jobs, L, nkv, hd);
+  else hipLaunchKernelGGL(kv_expand_kernel<float>, grid, dim3(256), 0, s, jobs, L, nkv, hd);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ eviction
+// A mass as an unsigned whole number of the same order: NaN 0, below -infinity; -0 as +0.
+__device__ __forceinline__ uint32_t mass_key(float m) {
+  uint32_t u = __float_as_uint(m);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
+  if (u == 0x80000000u) u = 0;
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// One block per (layer, KV head) row of a job: the `want` = keep - first - last
+// largest of its unprotected masses.  Four passes over the row find the key T of
+// the want-th largest, eight bits at a time (histogram of the keys that share
+// the bits found so far); a last pass lists the protected tokens, the keys above T
+// and the first ties at T, in order.
+__global__ void __launch_bounds__(256) kv_select_kernel(KvEvictJobs jobs, int rows) {
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t sh[2];
+  __shared__ uint32_t wsum[2][4];
+  const KvEvictJob &j = jobs.j[blockIdx.y];
+  const int row = blockIdx.x, P = j.P, keep = j.keep;
+  if (keep == 0) return;
+  const float *mass = j.mass + (size_t)row * P;
+  int32_t *kept = j.kept + (size_t)row * keep;
+  float *kmass = j.kept_mass ? j.kept_mass + (size_t)row * keep : nullptr;
+  const int lo = j.first, hi = P - j.last;
+  const uint32_t want = (uint32_t)(keep - j.first - j.last);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t T = 0, left = want;               // bits found; how many of the keys that share them are wanted
+  if (want > 0)
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      hist[tid] = 0;
+      __syncthreads();
+      const uint32_t above = shift == 24 ? 0u : ~0u << (shift + 8);
+      for (int i = lo + tid; i < hi; i += 256) {
+        const uint32_t k = mass_key(mass[i]);
+        if ((k & above) == T) atomicAdd(&hist[(k >> shift) & 255], 1u);
+      }
+      __syncthreads();
+      if (tid == 0) {
+        uint32_t acc = 0;
+        int d = 255;
+        for (; d > 0; --d) {
+          if (acc + hist[d] >= left) break;
+          acc += hist[d];
+        }
+        sh[0] = T | (uint32_t)d << shift;
+        sh[1] = left - acc;
+      }
+      __syncthreads();
+      T = sh[0];
+      left = sh[1];
+      __syncthreads();
+    }
+  // `left` of the keys equal to T are kept: those of the lowest indices
+  uint32_t ties = 0, out = 0;                // so far, over the whole block
+  for (int i0 = 0; i0 < P; i0 += 256) {
+    const int i = i0 + tid;
+    const float m = i < P ? mass[i] : 0.f;
+    const bool safe = i < P && (i < lo || i >= hi);
+    const uint32_t k = mass_key(m);
+    const bool cand = i < P && !safe && want > 0;
+    const bool tie = cand && k == T;
+    const uint64_t tb = __ballot(tie), below = (1ull << lane) - 1;
+    if (lane == 0) wsum[0][wave] = (uint32_t)__popcll(tb);
+    __syncthreads();
+    uint32_t trank = ties + (uint32_t)__popcll(tb & below);
+    uint32_t tall = ties;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) trank += wsum[0][w];
+      tall += wsum[0][w];
+    }
+    const bool take = safe || (cand && (k > T || (tie && trank < left)));
+    const uint64_t kb = __ballot(take);
+    if (lane == 0) wsum[1][wave] = (uint32_t)__popcll(kb);
+    __syncthreads();
+    uint32_t at = out + (uint32_t)__popcll(kb & below);
+    uint32_t oall = out;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) at += wsum[1][w];
+      oall += wsum[1][w];
+    }
+    if (take) {
+      kept[at] = i;
+      if (kmass) kmass[at] = m;
+    }
+    ties = tall;
+    out = oall;
+    __syncthreads();
+  }
+}
+
+// The kept tokens' rows (K and V): 16-byte pieces, `pieces` of them a row.  Rows of the
+// caches are [L][tokens][nkv]; destination row r = (layer keep + i) nkv + head.
+__global__ void __launch_bounds__(256) kv_gather_kernel(KvEvictJobs jobs, int L, int nkv, int pieces) {
+  const KvEvictJob &j = jobs.j[blockIdx.y];
+  const uint4 *src = reinterpret_cast<const uint4 *>(blockIdx.z ? j.sv : j.sk);
+  uint4 *dst = reinterpret_cast<uint4 *>(blockIdx.z ? j.dv : j.dk);
+  const size_t n = (size_t)L * j.keep * nkv * pieces;
+  for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < n; u += (size_t)gridDim.x * 256) {
+    const size_t r = u / pieces;
+    const int p = (int)(u - r * pieces);
+    const size_t t = r / nkv;                  // layer keep + i
+    const int h = (int)(r - t * nkv);
+    const size_t l = t / j.keep, i = t - l * j.keep;
+    const size_t tok = (size_t)j.kept[(l * nkv + h) * j.keep + i];
+    dst[u] = src[((l * j.P + tok) * nkv + h) * pieces + p];
+  }
+}
+
+// The scale bytes of 4-bit caches, `groups` a row.
+__global__ void __launch_bounds__(256) kv_gather_scales_kernel(KvEvictJobs jobs, int L, int nkv, int hd) {
+  const KvEvictJob &j = jobs.j[blockIdx.y];
+  const int groups = hd / kKvGroup;
+  const uint8_t *src = reinterpret_cast<const uint8_t *>(blockIdx.z ? j.sv : j.sk) + kv4_code_bytes(L, j.P, nkv, hd);
+  uint8_t *dst = reinterpret_cast<uint8_t *>(blockIdx.z ? j.dv : j.dk) + kv4_code_bytes(L, j.keep, nkv, hd);
+  const size_t n = (size_t)L * j.keep * nkv * groups;
+  for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < n; u += (size_t)gridDim.x * 256) {
+    const size_t r = u / groups;
+    const int p = (int)(u - r * groups);
+    const size_t t = r / nkv;
+    const int h = (int)(r - t * nkv);
+    const size_t l = t / j.keep, i = t - l * j.keep;
+    const size_t tok = (size_t)j.kept[(l * nkv + h) * j.keep + i];
+    dst[u] = src[((l * j.P + tok) * nkv + h) * groups + p];
+  }
+}
+
+hipError_t launch_kv_evict(const KvEvictJobs &jobs, int n, int L, int nkv, int hd, int esz, bool fp4, hipStream_t s) {
+  int most = 0;
+  for (int i = 0; i < n; ++i) most = std::max(most, jobs.j[i].keep);
+  if (n <= 0 || most == 0) return hipSuccess;
+  hipLaunchKernelGGL(kv_select_kernel, dim3(L * nkv, n), dim3(256), 0, s, jobs, L * nkv);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int pieces = (fp4 ? hd / 2 : hd * esz) / 16;
+  const size_t rows = (size_t)L * most * nkv;
+  hipLaunchKernelGGL(kv_gather_kernel, dim3(grid_x(rows * pieces, 4096), n, 2), dim3(256), 0, s, jobs, L, nkv, pieces);
+  e = hipGetLastError();
+  if (e != hipSuccess || !fp4) return e;
+  hipLaunchKernelGGL(kv_gather_scales_kernel, dim3(grid_x(rows * (hd / kKvGroup), 1024), n, 2), dim3(256), 0, s, jobs, L,
+                     nkv, hd);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ plain attention, either format
+// 16 consecutive elements of a row in fp32.
+template <typename T>
+__device__ __forceinline__ void load16(const T *p, float (&f)[16]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bf16x8 v = reinterpret_cast<const bf16x8 *>(p)[h];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[8 * h + q] = (float)v[q];
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const float4 v = reinterpret_cast<const float4 *>(p)[h];
+      f[4 * h] = v.x; f[4 * h + 1] = v.y; f[4 * h + 2] = v.z; f[4 * h + 3] = v.w;
+    }
+  }
+}
+// Elements 16 c .. 16 c + 15 of row `row` of a cache (rows of HD elements).
+template <int HD, typename T, bool FP4>
+__device__ __forceinline__ void load16_cache(const void *cache, size_t code_bytes, size_t row, int c, float (&f)[16]) {
+  if constexpr (FP4) {
+    const uint8_t *b = reinterpret_cast<const uint8_t *>(cache);
+    const uint2 w = *reinterpret_cast<const uint2 *>(b + row * (HD / 2) + c * 8);
+    const float s = kv4_scale(b[code_bytes + row * (HD / kKvGroup) + (c >> 1)]);
+    const bf16x8 v0 = kv4_bf16x8(w.x, s), v1 = kv4_bf16x8(w.y, s);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) { f[q] = (float)v0[q]; f[8 + q] = (float)v1[q]; }
+  } else {
+    load16(reinterpret_cast<const T *>(cache) + row * HD + c * 16, f);
+  }
+}
+template <int LG>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = 1; o < LG; o <<= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// One wave per query row.  LG = HD / 16 lanes hold a key (16 elements each), so 64 / LG
+// keys are under way at once, each lane group with a softmax of its own (running
+// maximum, sum, weighted values) over every (64 / LG)-th key; the groups join at the
+// end.  Everything in fp32.
+template <int HD, typename T, bool FP4>
+__global__ void __launch_bounds__(256) kv_attention_rows_kernel(KvAttnArgs ka) {
+  constexpr int LG = HD / 16, NG = 64 / LG;
+  const AttnArgs &a = ka.a;
+  const AttnItem it = a.items[blockIdx.x];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int qloc = blockIdx.y * 4 + wave;
+  if (qloc >= it.nq) return;
+  const int G = a.nq / a.nkv;
+  const int qrow = it.q0 + qloc;
+  const size_t row = (size_t)it.tok_off + qrow / G;
+  const int qg = it.kvh * G + qrow % G;
+  const int c = lane % LG, g = lane / LG;
+  const T *qkv = reinterpret_cast<const T *>(a.qkv);
+  float q[16], acc[16];
+  load16(qkv + row * a.ldqkv + (size_t)qg * HD + c * 16, q);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  const size_t codes = kv4_code_bytes(ka.L, it.P, a.nkv, HD);
+  const float scale = 1.0f / sqrtf((float)HD);
+  float m = -INFINITY, l = 0.f;
+  for (int k0 = it.kbeg; k0 < it.kend; k0 += NG) {
+    const int key = k0 + g;
+    const bool on = key < it.kend;
+    const int kk = on ? key : it.kend - 1;
+    float kf[16], vf[16];
+    if (kk < it.P) {
+      const size_t r = ((size_t)a.layer * it.P + kk) * a.nkv + it.kvh;
+      load16_cache<HD, T, FP4>(it.pk, codes, r, c, kf);
+      load16_cache<HD, T, FP4>(it.pv, codes, r, c, vf);
+    } else {
+      const T *p = qkv + ((size_t)it.tok_off + kk - it.P) * a.ldqkv + (size_t)(a.nq + it.kvh) * HD + c * 16;
+      load16(p, kf);
+      load16(p + (size_t)a.nkv * HD, vf);
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dot = fmaf(q[e], kf[e], dot);
+    dot = group_sum<LG>(dot) * scale;
+    if (!on) continue;
+    const float mn = fmaxf(m, dot), al = expf(m - mn), p = expf(dot - mn);
+    l = l * al + p;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = acc[e] * al + p * vf[e];
+    m = mn;
+  }
+  float mx = m;
+#pragma unroll
+  for (int o = LG; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+  const float w = l > 0.f || l != l ? expf(m - mx) : 0.f;   // a group without keys adds nothing
+  l *= w;
+#pragma unroll
+  for (int o = LG; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+  const float inv = 1.0f / l;
+  T *out = reinterpret_cast<T *>(a.o);
+  const size_t col = (size_t)qg * HD + c * 16;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float v = l == l && w == 0.f ? 0.f : acc[e] * w;
+#pragma unroll
+    for (int o = LG; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+    // row-major, or kb32
+    if (g == 0) out[a.o_rows > 0 ? kb32_offset(a.o_rows, row, col + e) : row * a.ldo + col + e] = from_f32<T>(v * inv);
+  }
+  if (ka.lse && lane == 0) ka.lse[row * a.nq + qg] = mx + logf(l);
+}
+
+template <int HD>
+static void launch_rows(const KvAttnArgs &a, bool bf16_mode, dim3 grid, hipStream_t s) {
+  if (bf16_mode) {
+    if (a.fp4) hipLaunchKernelGGL((kv_attention_rows_kernel<HD, bf16, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv_attention_rows_kernel<HD, bf16, false>), grid, dim3(256), 0, s, a);
+  } else {
+    if (a.fp4) hipLaunchKernelGGL((kv_attention_rows_kernel<HD, float, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv_attention_rows_kernel<HD, float, false>), grid, dim3(256), 0, s, a);
+  }
+}
+
+hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16_mode, hipStream_t s) {
+  if (a.a.n_items <= 0) return hipSuccess;
+  dim3 grid(a.a.n_items, kAttnQB / 4);
+  switch (a.a.hd) {
+    case 32: launch_rows<32>(a, bf16_mode, grid, s); break;
+    case 64: launch_rows<64>(a, bf16_mode, grid, s); break;
+    case 128: launch_rows<128>(a, bf16_mode, grid, s); break;
+    case 256: launch_rows<256>(a, bf16_mode, grid, s); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ attention weight of cached tokens
+// mass_j = sum over the KV head's query rows r of exp(q_r . k_j / sqrt(hd) - lse_r).  A
+// block holds kMassKeys keys, a wave one of them at a time; its lane groups take
+// every NG-th query row.
+template <int HD, typename T, bool FP4>
+__global__ void __launch_bounds__(256) kv_mass_rows_kernel(KvMassArgs a) {
+  constexpr int LG = HD / 16, NG = 64 / LG;
+  const MassItem it = a.items[blockIdx.x];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % LG, g = lane / LG;
+  const int G = a.nq / a.nkv, R = it.H * G;
+  const T *qkv = reinterpret_cast<const T *>(a.qkv);
+  const size_t codes = kv4_code_bytes(a.L, it.P, a.nkv, HD);
+  const float scale = 1.0f / sqrtf((float)HD);
+  for (int kk = wave; kk < it.nk; kk += 4) {
+    const int key = it.k0 + kk;
+    float kf[16];
+    load16_cache<HD, T, FP4>(it.pk, codes, ((size_t)a.layer * it.P + key) * a.nkv + it.kvh, c, kf);
+    float sum = 0.f;
+    for (int r0 = 0; r0 < R; r0 += NG) {
+      const int r = min(r0 + g, R - 1);
+      const size_t row = (size_t)it.tok_off + r / G;
+      const int qg = it.kvh * G + r % G;
+      float q[16];
+      load16(qkv + row * a.ldqkv + (size_t)qg * HD + c * 16, q);
+      float dot = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dot = fmaf(q[e], kf[e], dot);
+      dot = group_sum<LG>(dot) * scale;
+      if (r0 + g < R) sum += expf(dot - a.lse[row * a.nq + qg]);
+    }
+#pragma unroll
+    for (int o = LG; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) {
+      float *m = it.mass + ((size_t)a.layer * a.nkv + it.kvh) * it.P + key;
+      *m = a.accumulate ? *m + sum : sum;
+    }
+  }
+}
+
+template <int HD>
+static void launch_mass_rows(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
+  dim3 grid(a.n_items);
+  if (bf16_mode) {
+    if (a.fp4) hipLaunchKernelGGL((kv_mass_rows_kernel<HD, bf16, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv_mass_rows_kernel<HD, bf16, false>), grid, dim3(256), 0, s, a);
+  } else {
+    if (a.fp4) hipLaunchKernelGGL((kv_mass_rows_kernel<HD, float, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv_mass_rows_kernel<HD, float, false>), grid, dim3(256), 0, s, a);
+  }
+}
+
+hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
+  if (a.n_items <= 0) return hipSuccess;
+  switch (a.hd) {
+    case 32: launch_mass_rows<32>(a, bf16_mode, s); break;
+    case 64: launch_mass_rows<64>(a, bf16_mode, s); break;
+    case 128: launch_mass_rows<128>(a, bf16_mode, s); break;
+    case 256: launch_mass_rows<256>(a, bf16_mode, s); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace rosa

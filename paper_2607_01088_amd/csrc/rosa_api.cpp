@@ -14,6 +14,7 @@
 
 #include "../../include/rosa.h"
 #include "../../include/rosa_debug.h"
+#include "../../include/rosa_kv.h"
 #include "rosa_internal.h"
 #include "rosa_plan.h"
 
@@ -222,11 +223,11 @@ constexpr int kSmallCallRows = 1024;
 
 enum KernelClass {
   kcTime = 0, kcSetup, kcInProj, kcModNorm, kcGemmQKV, kcAttention, kcMerge, kcGemmO, kcGemmUp,
-  kcGemmDown, kcFinal, kcCount
+  kcGemmDown, kcFinal, kcMass, kcCount
 };
 const char *kClassNames[kcCount] = {"time_conditioning", "setup_rows", "in_proj", "modnorm", "gemm_qkv",
                                     "attention", "attn_merge", "gemm_o", "gemm_up", "gemm_down",
-                                    "final_euler"};
+                                    "final_euler", "kv_mass"};
 
 thread_local std::string g_create_error;
 
@@ -265,6 +266,7 @@ struct rosa_batch {
   int32_t *row_req = nullptr, *rowmod = nullptr, *ident = nullptr;
   float *modtab = nullptr, *emb = nullptr, *tc1 = nullptr, *tc2 = nullptr, *gemv_ws = nullptr;
   float *part_o = nullptr, *part_ml = nullptr;
+  float *lse = nullptr;              // log-sum-exp of the step's attention rows, [row][n_q] (masses)
   float *gemm_part = nullptr;        // K-slice products of split projections (one lane only)
   size_t gemm_part_floats = 0;
   // bf16 deferred norms (unsplit output projection and MLP-down): per row the
@@ -283,7 +285,8 @@ struct rosa_batch {
   int plan_flip = 0;
   size_t plan_bytes = 0;
   size_t off_reqs = 0, off_tau_idx = 0, off_taus = 0, off_items = 0, off_groups = 0, off_lists = 0;
-  size_t max_list_ints = 0;
+  size_t off_mass = 0;               // mass items (rosa_generate_kv)
+  size_t max_list_ints = 0, max_mass = 0;
 
   std::vector<void *> allocations;
 
@@ -657,11 +660,21 @@ int call_lanes(const rosa_capacity &cap, const rosa_request *reqs, int n, int ma
   return k_max > 0 && row_steps >= kMinTwoLaneRows * (double)k_max ? 2 : 1;
 }
 
+// What rosa_generate_kv adds to a call: the format of its prefix caches and, with
+// masses, the work of gathering them (items of plan requests [0, r] in upto[r]).
+struct KvUse {
+  bool fp4 = false, gather = false;
+  std::vector<MassItem> items;
+  std::vector<int32_t> upto;
+  bool plain() const { return !fp4 && !gather; }
+};
+
 // Copy the plan through a pinned staging buffer into the device plan region.
-hipError_t upload_plan(rosa_batch *b, const Plan &p, const rosa_request *reqs, int n) {
+hipError_t upload_plan(rosa_batch *b, const Plan &p, const rosa_request *reqs, int n, const KvUse &kv = KvUse()) {
   const Plan::AttnSet &S0 = p.sets[0], &S1 = p.sets[1];
   const size_t n_items = S0.items.size() + S1.items.size(), n_groups = S0.groups.size() + S1.groups.size();
-  if ((int64_t)n_items > b->max_items || (int64_t)n_groups > b->max_slots || p.attn_lists.size() > b->max_list_ints)
+  if ((int64_t)n_items > b->max_items || (int64_t)n_groups > b->max_slots || p.attn_lists.size() > b->max_list_ints ||
+      kv.items.size() > b->max_mass)
     return hipErrorInvalidValue;
   const int slot = b->plan_flip;
   b->plan_flip ^= 1;
@@ -694,6 +707,12 @@ hipError_t upload_plan(rosa_batch *b, const Plan &p, const rosa_request *reqs, i
   const size_t used = b->off_lists + p.attn_lists.size() * sizeof(AttnItem);
   hipError_t e = hipMemcpyAsync(b->d_plan, hp, used, hipMemcpyHostToDevice, b->stream);
   if (e != hipSuccess) return e;
+  if (!kv.items.empty()) {
+    std::memcpy(hp + b->off_mass, kv.items.data(), kv.items.size() * sizeof(MassItem));
+    e = hipMemcpyAsync((uint8_t *)b->d_plan + b->off_mass, hp + b->off_mass, kv.items.size() * sizeof(MassItem),
+                       hipMemcpyHostToDevice, b->stream);
+    if (e != hipSuccess) return e;
+  }
   e = hipEventRecord(b->plan_copied[slot], b->stream);
   b->plan_pending[slot] = true;
   return e;
@@ -718,7 +737,8 @@ hipError_t run_time_conditioning(rosa_batch *b, const float *d_taus, int n_tau, 
 
 // Attention of one layer for the requests active at step k of lane ln.
 hipError_t run_attention(rosa_batch *b, const Plan &p, const Plan::Lane &ln, int k, int layer, const void *qkv,
-                         void *o, hipStream_t st, int o_rows, const WeightPrefetch *prefetch = nullptr) {
+                         void *o, hipStream_t st, int o_rows, const WeightPrefetch *prefetch = nullptr,
+                         const KvUse *kv = nullptr) {
   const Dims &D = b->dims;
   const ReqDesc *reqs = (const ReqDesc *)((uint8_t *)b->d_plan + b->off_reqs);
   const AttnItem *items = (const AttnItem *)((uint8_t *)b->d_plan + b->off_items);
@@ -746,6 +766,22 @@ hipError_t run_attention(rosa_batch *b, const Plan &p, const Plan::Lane &ln, int
   a.qkv = qkv; a.ldqkv = D.qkv_dim; a.o = o; a.ldo = D.o_dim; a.o_rows = o_rows;
   a.nq = D.nq; a.nkv = D.nkv; a.hd = D.hd;
   a.part_o = b->part_o; a.part_ml = b->part_ml;
+  if (kv && !kv->plain()) {
+    KvAttnArgs ka{};
+    ka.a = a; ka.a.items = items + it_lo;
+    ka.L = D.L; ka.fp4 = kv->fp4; ka.lse = kv->gather && v == 0 ? b->lse : nullptr;
+    hipError_t e = timed(b, kcAttention, [&] { return launch_kv_attention_rows(ka, b->bf16, st); });
+    const int m_lo = kv->gather && r0 > 0 ? kv->upto[r0 - 1] : 0, m_hi = kv->gather ? kv->upto[r0 + n_act - 1] : 0;
+    if (e != hipSuccess || v != 0 || m_hi == m_lo) return e;
+    KvMassArgs ma{};
+    ma.items = (const MassItem *)((uint8_t *)b->d_plan + b->off_mass) + m_lo;
+    ma.n_items = m_hi - m_lo;
+    ma.layer = layer; ma.L = D.L;
+    ma.qkv = qkv; ma.ldqkv = D.qkv_dim; ma.lse = b->lse;
+    ma.nq = D.nq; ma.nkv = D.nkv; ma.hd = D.hd;
+    ma.fp4 = kv->fp4; ma.accumulate = true;
+    return timed(b, kcMass, [&] { return launch_kv_mass(ma, b->bf16, st); });
+  }
   hipError_t e = timed(b, kcAttention, [&] { return launch_attention(a, b->bf16, st); });
   if (e == hipSuccess && gr_hi > gr_lo)
     e = timed(b, kcMerge, [&] {
@@ -753,6 +789,27 @@ hipError_t run_attention(rosa_batch *b, const Plan &p, const Plan::Lane &ln, int
                                D.hd, b->bf16, st, o_rows);
     });
   return e;
+}
+
+// The checks and mass items of a rosa_generate_kv call, in plan order.
+rosa_status plan_kv(rosa_batch *b, const Plan &p, const rosa_request *reqs, int n, float *const *mass, KvUse &kv) {
+  for (int i = 0; i < n; ++i) {
+    if (((uintptr_t)reqs[i].prefix_k | (uintptr_t)reqs[i].prefix_v) & 15)
+      return fail(b, ROSA_E_INVALID, "a prefix cache is not 16-byte aligned");
+    if (mass && reqs[i].prefix_len > 0 && (!mass[i] || (uintptr_t)mass[i] & 3))
+      return fail(b, ROSA_E_INVALID, "a request's masses are NULL or not 4-byte aligned");
+  }
+  if (!mass) return ROSA_OK;
+  kv.upto.resize(n);
+  for (int i = 0; i < n; ++i) {
+    const rosa_request &r = reqs[p.order[i]];
+    for (int kvh = 0; kvh < b->dims.nkv; ++kvh)
+      for (int k0 = 0; k0 < r.prefix_len; k0 += kMassKeys)
+        kv.items.push_back({r.prefix_k, mass[p.order[i]], r.prefix_len, r.horizon, p.tok_off[i], kvh, k0,
+                            std::min(kMassKeys, r.prefix_len - k0), {0, 0}});
+    kv.upto[i] = (int32_t)kv.items.size();
+  }
+  return ROSA_OK;
 }
 
 void free_all(rosa_batch *b) {
@@ -926,6 +983,7 @@ rosa_status rosa_batch_create(const rosa_model_config *cfg, const rosa_weights *
     }
     b->part_o = dalloc<float>(b, (size_t)b->max_slots * kAttnQB * D.hd, e);
     b->part_ml = dalloc<float>(b, (size_t)b->max_slots * kAttnQB * 2, e);
+    b->lse = dalloc<float>(b, maxM * D.nq, e);
 
     // plan region
     const int G = D.nq / D.nkv;
@@ -941,7 +999,9 @@ rosa_status rosa_batch_create(const rosa_model_config *cfg, const rosa_weights *
     // one launch order per step and lane at most: its items plus at most as
     // many idle first entries (n_blocks <= items + 7)
     b->max_list_ints = (size_t)cap->max_steps * (2 * (size_t)b->max_items + 8 * kMaxLanes * n_sets);
-    b->plan_bytes = align(b->off_lists + b->max_list_ints * sizeof(AttnItem));
+    b->off_mass = align(b->off_lists + b->max_list_ints * sizeof(AttnItem));
+    b->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassKeys) + (size_t)cap->max_requests);
+    b->plan_bytes = align(b->off_mass + b->max_mass * sizeof(MassItem));
     b->d_plan = dalloc<uint8_t>(b, b->plan_bytes, e);
     if (e != hipSuccess) {
       rosa_status s2 = e == hipErrorOutOfMemory ? fail(nullptr, ROSA_E_NOMEM, "device allocation failed")
@@ -1004,20 +1064,29 @@ rosa_status rosa_generate_actions(rosa_batch *b, const rosa_request *reqs, int32
   return rosa_generate_steps(b, reqs, n, INT32_MAX);
 }
 
-rosa_status rosa_generate_steps(rosa_batch *b, const rosa_request *reqs, int32_t n, int32_t max_steps) {
+static rosa_status generate(rosa_batch *b, const rosa_request *reqs, int32_t n, int32_t max_steps, int32_t format,
+                            float *const *mass) {
   if (!b) return ROSA_E_INVALID;
   try {
     b->last_error.clear();
     if (b->poisoned) return fail(b, ROSA_E_DEVICE, "handle is poisoned by an earlier device error");
+    if (format != ROSA_KV_MODEL && format != ROSA_KV_FP4) return fail(b, ROSA_E_INVALID, "unknown cache format");
+    KvUse kv;
+    kv.fp4 = format == ROSA_KV_FP4;
+    kv.gather = mass != nullptr;
     Plan p;
     std::string err;
     // Lanes only without per-kernel profiling (its events live on one stream).
     const int lanes = b->prof ? 1 : call_lanes(b->cap, reqs, n, max_steps, b->lanes);
-    rosa_status st = build_plan(&b->cfg, &b->cap, reqs, n, true, b->bf16, lanes, p, err, max_steps);
+    rosa_status st = build_plan(&b->cfg, &b->cap, reqs, n, true, b->bf16 && kv.plain(), lanes, p, err, max_steps);
     if (st != ROSA_OK) return fail(b, st, err);
     if (n == 0) return ROSA_OK;
+    if (!kv.plain()) {
+      st = plan_kv(b, p, reqs, n, mass, kv);
+      if (st != ROSA_OK) return st;
+    }
     hipError_t e = hipSetDevice(b->device);
-    if (e == hipSuccess) e = upload_plan(b, p, reqs, n);
+    if (e == hipSuccess) e = upload_plan(b, p, reqs, n, kv);
     if (e != hipSuccess) return device_fail(b, e, "plan upload");
     const Dims &D = b->dims;
     uint8_t *dp = (uint8_t *)b->d_plan;
@@ -1137,7 +1206,7 @@ rosa_status rosa_generate_steps(rosa_batch *b, const rosa_request *reqs, int32_t
               {(uint8_t *)b->wt_up + (size_t)l * D.dff * D.d * es, D.d / 32, (uint32_t)D.dff * 64},
               {(uint8_t *)b->wt_down + (size_t)l * D.d * D.dff * es, D.dff / 32, (uint32_t)D.d * 64},
               {(uint8_t *)b->wt_qkv + (size_t)lq * D.qkv_dim * D.d * es, D.d / 32, (uint32_t)D.qkv_dim * 64}};
-          e = run_attention(b, p, ln, k, l, b->qkv, b->o, st, b->kb_rows, prefetch_ok(M) ? pf : nullptr);
+          e = run_attention(b, p, ln, k, l, b->qkv, b->o, st, b->kb_rows, prefetch_ok(M) ? pf : nullptr, &kv);
           if (e != hipSuccess) break;
           GemmArgs go{};
           if (split_ok) { go.part = b->gemm_part; go.part_floats = b->gemm_part_floats; }
@@ -1216,6 +1285,15 @@ rosa_status rosa_generate_steps(rosa_batch *b, const rosa_request *reqs, int32_t
   } catch (...) {
     return fail(b, ROSA_E_DEVICE, "unexpected exception");
   }
+}
+
+rosa_status rosa_generate_steps(rosa_batch *b, const rosa_request *reqs, int32_t n, int32_t max_steps) {
+  return generate(b, reqs, n, max_steps, ROSA_KV_MODEL, nullptr);
+}
+
+rosa_status rosa_generate_kv(rosa_batch *b, const rosa_request *reqs, int32_t n, int32_t max_steps, int32_t format,
+                             float *const *mass) {
+  return generate(b, reqs, n, max_steps, format, mass);
 }
 
 void rosa_destroy(rosa_batch *b) {

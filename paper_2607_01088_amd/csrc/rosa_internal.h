@@ -272,4 +272,65 @@ hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const ReqDes
                              const void *part_o, const float *part_ml, void *o, int ldo, int nq,
                              int nkv, int hd, bool bf16, hipStream_t s, int o_rows = 0);
 
+// ------------------------------------------------------------------ 4-bit caches and eviction
+// One 4-bit cache (K or V of one request): codes [L][P][nkv][hd / 2] bytes, then
+// scale bytes [L][P][nkv][hd / 32].
+constexpr int kKvGroup = 32;       // elements that share a scale
+__host__ __device__ inline size_t kv4_code_bytes(size_t L, size_t P, size_t nkv, size_t hd) { return L * P * nkv * (hd / 2); }
+__host__ __device__ inline size_t kv4_bytes(size_t L, size_t P, size_t nkv, size_t hd) {
+  return kv4_code_bytes(L, P, nkv, hd) + L * P * nkv * (hd / kKvGroup);
+}
+
+// Caches to convert, passed by value (so a call needs no device memory and a
+// captured launch keeps them).
+struct KvJob { const void *sk, *sv; void *dk, *dv; int32_t P, pad; };
+constexpr int kKvJobs = 64;        // per launch
+struct KvJobs { KvJob j[kKvJobs]; };
+hipError_t launch_kv_quantize(const KvJobs &jobs, int n, int L, int nkv, int hd, bool bf16, hipStream_t s);
+hipError_t launch_kv_expand(const KvJobs &jobs, int n, int L, int nkv, int hd, bool bf16, hipStream_t s);
+
+struct KvEvictJob {
+  const void *sk, *sv;
+  void *dk, *dv;
+  const float *mass;
+  int32_t *kept;
+  float *kept_mass;
+  int32_t P, keep, first, last;
+};
+constexpr int kKvEvictJobs = 32;   // per launch
+struct KvEvictJobs { KvEvictJob j[kKvEvictJobs]; };
+// fp4: 4-bit caches, else rows of hd elements of esz bytes.
+hipError_t launch_kv_evict(const KvEvictJobs &jobs, int n, int L, int nkv, int hd, int esz, bool fp4, hipStream_t s);
+
+// Attention over caches in either format, fp32 sums throughout (`bf16`: the
+// type of qkv, o and model-type caches); items are not split over keys.
+// lse: [stacked row][nq], or NULL.
+struct KvAttnArgs {
+  AttnArgs a;
+  int L;                 // layers of the caches
+  bool fp4;
+  float *lse;
+};
+hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16, hipStream_t s);
+
+// Keys [k0, k0 + nk) of one KV head of one request, whose attention weight
+// is summed over the request's H action tokens (nk <= kMassKeys).
+struct MassItem {
+  const void *pk;        // the request's K cache
+  float *mass;           // [L][nkv][P]
+  int32_t P, H, tok_off, kvh, k0, nk;
+  int32_t pad[2];
+};
+static_assert(sizeof(MassItem) == 48, "MassItem is 48 bytes");
+constexpr int kMassKeys = 32;
+struct KvMassArgs {
+  const MassItem *items; int n_items;
+  int layer, L;
+  const void *qkv; int ldqkv;
+  const float *lse;      // [stacked row][nq]
+  int nq, nkv, hd;
+  bool fp4, accumulate;
+};
+hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16, hipStream_t s);
+
 }  // namespace rosa

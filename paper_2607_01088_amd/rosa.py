@@ -1,5 +1,5 @@
 """Python binding of the rosa C ABI (include/rosa.h, rosa_prefill.h, rosa_sched.h,
-rosa_debug.h).
+rosa_kv.h, rosa_debug.h).
 
 Argument marshalling only: every step of the computation runs in the HIP
 library.  PyTorch supplies device memory and the stream.  The library must be
@@ -74,6 +74,20 @@ class VlmWeights(C.Structure):
 class PrefixJob(C.Structure):
     _fields_ = [("embeddings", C.c_void_p), ("prefix_k", C.c_void_p), ("prefix_v", C.c_void_p),
                 ("prefix_len", C.c_int32), ("causal_len", C.c_int32)]
+
+
+ROSA_KV_MODEL, ROSA_KV_FP4 = 0, 1
+
+
+class KvJob(C.Structure):
+    _fields_ = [("src_k", C.c_void_p), ("src_v", C.c_void_p), ("dst_k", C.c_void_p), ("dst_v", C.c_void_p),
+                ("prefix_len", C.c_int32), ("reserved", C.c_int32)]
+
+
+class KvEvictJob(C.Structure):
+    _fields_ = [("src_k", C.c_void_p), ("src_v", C.c_void_p), ("dst_k", C.c_void_p), ("dst_v", C.c_void_p),
+                ("mass", C.c_void_p), ("kept", C.c_void_p), ("kept_mass", C.c_void_p), ("prefix_len", C.c_int32),
+                ("keep", C.c_int32), ("first", C.c_int32), ("last", C.c_int32)]
 
 
 class RatePoint(C.Structure):
@@ -200,6 +214,27 @@ def load(path: Optional[str] = None) -> C.CDLL:
     lib.rosa_schedule_homogeneous.argtypes = [C.POINTER(Fleet), C.POINTER(ModelProfile), i32,
                                               C.POINTER(FleetSchedule), C.POINTER(ServerPlan)]
     lib.rosa_schedule_homogeneous.restype = C.c_int
+    lib.rosa_generate_kv.argtypes = [vp, C.POINTER(Request), i32, i32, i32, C.POINTER(vp)]
+    lib.rosa_generate_kv.restype = C.c_int
+    lib.rosa_kv_bytes.argtypes = [C.POINTER(ModelConfig), i32, i32]
+    lib.rosa_kv_bytes.restype = i64
+    for f in (lib.rosa_kv_quantize, lib.rosa_kv_expand):
+        f.argtypes = [C.POINTER(ModelConfig), C.POINTER(KvJob), i32, vp]
+        f.restype = C.c_int
+    lib.rosa_kv_evict.argtypes = [C.POINTER(ModelConfig), i32, C.POINTER(KvEvictJob), i32, vp]
+    lib.rosa_kv_evict.restype = C.c_int
+    lib.rosa_kv_create.argtypes = [C.POINTER(ModelConfig), C.POINTER(Capacity), vp, C.POINTER(vp)]
+    lib.rosa_kv_create.restype = C.c_int
+    lib.rosa_kv_plan.argtypes = [vp, C.POINTER(Request), i32, i32, C.POINTER(vp)]
+    lib.rosa_kv_plan.restype = C.c_int
+    lib.rosa_kv_attention.argtypes = [vp, i32, vp, vp, vp]
+    lib.rosa_kv_attention.restype = C.c_int
+    lib.rosa_kv_mass.argtypes = [vp, i32, vp, vp, i32]
+    lib.rosa_kv_mass.restype = C.c_int
+    lib.rosa_kv_destroy.argtypes = [vp]
+    lib.rosa_kv_destroy.restype = None
+    lib.rosa_kv_last_error.argtypes = [vp]
+    lib.rosa_kv_last_error.restype = C.c_char_p
     _lib = lib
     return lib
 
@@ -416,6 +451,15 @@ class ActionExpert:
         self._check(st)
         return st
 
+    def generate_kv(self, reqs: Sequence[Request], fmt: int, max_steps: int = 2 ** 31 - 1,
+                    mass: Optional[Sequence] = None) -> None:
+        """rosa_generate_kv: steps over prefix caches in format ROSA_KV_*; mass: one tensor
+        or device pointer per request, [L][n_kv][P] fp32, added to."""
+        if mass is not None and len(mass) != len(reqs):
+            raise ValueError("one mass array per request")
+        self._check(self.lib.rosa_generate_kv(self.handle, request_array(reqs), len(reqs), max_steps, fmt,
+                                              _mass_array(mass)))
+
     def generate_status(self, reqs: Sequence[Request]) -> int:
         """Like generate but returns the status instead of raising."""
         arr = request_array(reqs)
@@ -554,6 +598,110 @@ class PrefixProducer:
     def close(self) -> None:
         if getattr(self, "handle", None):
             self.lib.rosa_prefill_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------- prefix-cache operators
+
+def _ptr(t):
+    return t if t is None or isinstance(t, int) else t.data_ptr()
+
+
+def _stream(stream: Optional[int]) -> int:
+    if stream is not None:
+        return stream
+    import torch
+    return torch.cuda.current_stream().cuda_stream
+
+
+def kv_bytes(shape, dtype: str, fmt: int, P: int) -> int:
+    """Bytes of one cache (K or V) of P tokens in format ROSA_KV_* (rosa_kv_bytes)."""
+    cfg = model_config(shape, dtype)
+    n = load().rosa_kv_bytes(C.byref(cfg), fmt, P)
+    if n < 0:
+        raise RosaError(ROSA_E_INVALID, "rosa_kv_bytes: invalid configuration, format or length")
+    return n
+
+
+def kv_jobs(jobs: Sequence[tuple]):
+    """Conversion jobs from (src_k, src_v, dst_k, dst_v, prefix_len) tuples of tensors
+    or raw device pointers; one list serves any number of calls."""
+    return (KvJob * max(1, len(jobs)))(*[KvJob(*[_ptr(x) for x in j[:4]], j[4], 0) for j in jobs]), len(jobs)
+
+
+def kv_evict_jobs(jobs: Sequence[tuple]):
+    """Eviction jobs from (src_k, src_v, dst_k, dst_v, mass, kept, kept_mass, prefix_len,
+    keep, first, last) tuples of tensors or raw device pointers."""
+    return (KvEvictJob * max(1, len(jobs)))(*[KvEvictJob(*[_ptr(x) for x in j[:7]], *j[7:]) for j in jobs]), len(jobs)
+
+
+def _kv_call(st: int) -> None:
+    if st != ROSA_OK:
+        raise RosaError(st, load().rosa_kv_last_error(None).decode())
+
+
+def kv_quantize(shape, dtype: str, jobs, stream: Optional[int] = None) -> None:
+    """Prefix caches in the model dtype to 4 bits (rosa_kv_quantize); jobs from kv_jobs."""
+    cfg = model_config(shape, dtype)
+    _kv_call(load().rosa_kv_quantize(C.byref(cfg), jobs[0], jobs[1], _stream(stream)))
+
+
+def kv_expand(shape, dtype: str, jobs, stream: Optional[int] = None) -> None:
+    """4-bit prefix caches to the model dtype (rosa_kv_expand); jobs from kv_jobs."""
+    cfg = model_config(shape, dtype)
+    _kv_call(load().rosa_kv_expand(C.byref(cfg), jobs[0], jobs[1], _stream(stream)))
+
+
+def kv_evict(shape, dtype: str, fmt: int, jobs, stream: Optional[int] = None) -> None:
+    """Keep the cached tokens of the largest mass (rosa_kv_evict); jobs from kv_evict_jobs."""
+    cfg = model_config(shape, dtype)
+    _kv_call(load().rosa_kv_evict(C.byref(cfg), fmt, jobs[0], jobs[1], _stream(stream)))
+
+
+def _mass_array(mass: Optional[Sequence]):
+    return None if mass is None else (C.c_void_p * max(1, len(mass)))(*[_ptr(m) for m in mass])
+
+
+class KvAttention:
+    """A rosa_kv handle: the planned attention of a request set over prefix caches in
+    either format, and the attention weight of their tokens."""
+
+    def __init__(self, shape, dtype: str, cap: Capacity, stream: Optional[int] = None):
+        self.lib = load()
+        self.shape, self.dtype, self.cap = shape, dtype, cap
+        self._cfg = model_config(shape, dtype)
+        self.stream = _stream(stream)
+        h = C.c_void_p()
+        _kv_call(self.lib.rosa_kv_create(C.byref(self._cfg), C.byref(cap), self.stream, C.byref(h)))
+        self.handle = h
+
+    def _check(self, st: int):
+        if st != ROSA_OK:
+            raise RosaError(st, self.lib.rosa_kv_last_error(self.handle).decode())
+
+    def plan(self, reqs: Sequence[Request], fmt: int, mass: Optional[Sequence] = None) -> None:
+        """rosa_kv_plan; mass: one tensor or device pointer per request, [L][n_kv][P] fp32."""
+        if mass is not None and len(mass) != len(reqs):
+            raise ValueError("one mass array per request")
+        self._check(self.lib.rosa_kv_plan(self.handle, request_array(reqs), len(reqs), fmt, _mass_array(mass)))
+
+    def attention(self, layer: int, qkv, o, lse=None) -> None:
+        """rosa_kv_attention on torch tensors; lse: fp32 [rows][n_q] or None."""
+        self._check(self.lib.rosa_kv_attention(self.handle, layer, qkv.data_ptr(), o.data_ptr(), _ptr(lse)))
+
+    def mass(self, layer: int, qkv, lse, accumulate: bool = True) -> None:
+        """rosa_kv_mass: adds to (or, accumulate False, replaces) the planned masses of a layer."""
+        self._check(self.lib.rosa_kv_mass(self.handle, layer, qkv.data_ptr(), lse.data_ptr(), 1 if accumulate else 0))
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            self.lib.rosa_kv_destroy(self.handle)
             self.handle = None
 
     def __del__(self):
