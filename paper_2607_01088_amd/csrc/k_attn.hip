@@ -33,28 +33,9 @@ namespace rosa {
 
 namespace at {
 constexpr int TK = 32;   // keys per LDS stage
-constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 constexpr int waitcnt_lgkm0 = 15 | (3 << 14) | (7 << 4);   // lgkmcnt(0), others unconstrained
-// Chunk swizzle of LDS rows: 16-byte chunk c of row r is stored at c ^ swz(r),
-// swz(r) = the two 2-bit halves of r % 16 swapped.  The 16 consecutive rows
-// that one 16-lane group reads at one chunk (K operand), and the 4 rows x 4
-// chunks that the transpose reads of a 32-lane half touch (V operand), then
-// fall in distinct bank groups.
-__device__ __forceinline__ int swz(int r, int cpr) { return (((r & 3) << 2) | ((r >> 2) & 3)) & (cpr - 1); }
 }  // namespace at
 
-
-
-typedef __attribute__((address_space(3))) const uint8_t lds_u8;
-__device__ __forceinline__ const lds_u8 *lds_ptr(uint32_t a) { return (const lds_u8 *)(size_t)a; }
-__device__ __forceinline__ bf16x8 lds_tr_pair(const lds_u8 *p0, const lds_u8 *p1) {
-  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-  const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p0));
-  const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p1));
-  const uint2 u0 = __builtin_bit_cast(uint2, v0);
-  const uint2 u1 = __builtin_bit_cast(uint2, v1);
-  return __builtin_bit_cast(bf16x8, make_uint4(u0.x, u0.y, u1.x, u1.y));
-}
 template <int HD, int NG>
 struct AttnTile {
   static constexpr int ROWB = HD * 2;             // bytes per K or V row
@@ -104,7 +85,10 @@ __device__ __forceinline__ void prefetch_weights(const WeightPrefetch (&pf)[kPre
 // CAUSAL: the prefix producer's launches with causal segments; each query
 // row additionally masks the keys at or past its token's limit
 // max(causal_b, t + 1) in the tiles that reach it.
-template <int HD, int NG, bool CAUSAL>
+// LSE: the rows' log-sum-exp goes to a.lse; the softmax sums are then taken in fp32
+// before the weights are rounded to bf16 (sums of rounded weights would leave a
+// log-sum-exp of bf16's accuracy).
+template <int HD, int NG, bool CAUSAL, bool LSE>
 __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
   using at::TK;
   using T = AttnTile<HD, NG>;
@@ -380,7 +364,8 @@ __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
           bf16x2 p2;
           p2[0] = (bf16)s[g][8 * h + 2 * e];
           p2[1] = (bf16)s[g][8 * h + 2 * e + 1];
-          ps = __builtin_amdgcn_fdot2_f32_bf16(p2, ones, ps, false);
+          if constexpr (LSE) ps += s[g][8 * h + 2 * e] + s[g][8 * h + 2 * e + 1];
+          else ps = __builtin_amdgcn_fdot2_f32_bf16(p2, ones, ps, false);
           w[e] = __builtin_bit_cast(uint32_t, p2);
         }
         pp[g][h] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
@@ -536,6 +521,11 @@ __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
       pm[0] = m_ref[g] * sl2;       // log2 units, as the merge expects
       pm[1] = l_all;
     }
+    if constexpr (LSE) {
+      const int qrow = it.q0 + loc;
+      if (it.slot < 0 && half == 0)
+        a.lse[(size_t)(it.tok_off + qrow / G) * a.nq + it.kvh * G + qrow % G] = (m_ref[g] * sl2 + log2f(l_all)) * 0.6931471805599453f;
+    }
   }
   __builtin_amdgcn_s_waitcnt(at::waitcnt_lgkm0);   // this wave's staging writes are done
 #pragma unroll
@@ -632,16 +622,16 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(AttnArgs a) {
 // (O_c in bf16, m_c and l_c in fp32).
 template <typename OutT>
 __global__ void __launch_bounds__(256) attn_merge_kernel(const AttnGroup *__restrict__ groups,
-                                                         const ReqDesc *__restrict__ reqs,
                                                          const bf16 *__restrict__ part_o,
                                                          const float *__restrict__ part_ml, OutT *o,
-                                                         int ldo, int nq, int nkv, int hd, int o_rows) {
+                                                         int ldo, int nq, int nkv, int hd, int o_rows,
+                                                         float *lse) {
   const AttnGroup gr = groups[blockIdx.y];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int qloc = blockIdx.x * 4 + wave;
   const int G = nq / nkv;
   if (qloc >= gr.nq) return;
-  const int tok_off = reqs[gr.req].tok_off;   // issued now, used for the store
+  const int tok_off = gr.tok_off;
   const int qrow = gr.q0 + qloc;
   const int qt = qrow / G, qg = gr.kvh * G + qrow % G;
   // Partials are read CH slots at a time (their max and sum with their O),
@@ -682,6 +672,7 @@ __global__ void __launch_bounds__(256) attn_merge_kernel(const AttnGroup *__rest
     }
     mx = nm;
   }
+  if (lse && lane == 0) lse[(size_t)(tok_off + qt) * nq + qg] = (mx + log2f(L)) * 0.6931471805599453f;
   if (!on) return;
   const float inv = 1.0f / L;
   const size_t orow = (size_t)(tok_off + qt), col = (size_t)qg * hd + e0;
@@ -691,30 +682,27 @@ __global__ void __launch_bounds__(256) attn_merge_kernel(const AttnGroup *__rest
 }
 
 
+template <int HD>
+static void launch_bf16(const AttnArgs &a, dim3 grid, hipStream_t s) {
+  constexpr int NG = attn_groups_per_wave(HD);
+  if (a.causal) hipLaunchKernelGGL((attention_bf16_kernel<HD, NG, true, false>), grid, dim3(256), 0, s, a);
+  else if (a.lse) hipLaunchKernelGGL((attention_bf16_kernel<HD, NG, false, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attention_bf16_kernel<HD, NG, false, false>), grid, dim3(256), 0, s, a);
+}
+
 hipError_t launch_attention(const AttnArgs &a, bool bf16_mode, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
   if (a.o_rows > 0 && !bf16_mode) return hipErrorInvalidValue;
+  if (a.lse && (a.causal || !bf16_mode)) return hipErrorInvalidValue;
   if (bf16_mode) {
     if (a.n_blocks <= 0) return hipSuccess;
     if (a.n_prefetch < 0 || a.n_prefetch % 8 || (a.n_prefetch > 0 && a.n_blocks % 8)) return hipErrorInvalidValue;
     dim3 grid(a.n_blocks + a.n_prefetch);
     switch (a.hd) {
-      case 32:
-        if (a.causal) hipLaunchKernelGGL((attention_bf16_kernel<32, attn_groups_per_wave(32), true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((attention_bf16_kernel<32, attn_groups_per_wave(32), false>), grid, dim3(256), 0, s, a);
-        break;
-      case 64:
-        if (a.causal) hipLaunchKernelGGL((attention_bf16_kernel<64, attn_groups_per_wave(64), true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((attention_bf16_kernel<64, attn_groups_per_wave(64), false>), grid, dim3(256), 0, s, a);
-        break;
-      case 128:
-        if (a.causal) hipLaunchKernelGGL((attention_bf16_kernel<128, attn_groups_per_wave(128), true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((attention_bf16_kernel<128, attn_groups_per_wave(128), false>), grid, dim3(256), 0, s, a);
-        break;
-      case 256:
-        if (a.causal) hipLaunchKernelGGL((attention_bf16_kernel<256, attn_groups_per_wave(256), true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((attention_bf16_kernel<256, attn_groups_per_wave(256), false>), grid, dim3(256), 0, s, a);
-        break;
+      case 32: launch_bf16<32>(a, grid, s); break;
+      case 64: launch_bf16<64>(a, grid, s); break;
+      case 128: launch_bf16<128>(a, grid, s); break;
+      case 256: launch_bf16<256>(a, grid, s); break;
       default: return hipErrorInvalidValue;
     }
   } else {
@@ -730,19 +718,18 @@ hipError_t launch_attention(const AttnArgs &a, bool bf16_mode, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const ReqDesc *reqs,
-                             const void *part_o, const float *part_ml, void *o, int ldo, int nq,
-                             int nkv, int hd, bool bf16_mode, hipStream_t s, int o_rows) {
+hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const void *part_o, const float *part_ml, void *o, int ldo, int nq,
+                             int nkv, int hd, bool bf16_mode, hipStream_t s, int o_rows, float *lse) {
   if (n_groups <= 0) return hipSuccess;
   if (hd > 256) return hipErrorInvalidValue;   // a lane holds at most 4 head-dim elements
   if (o_rows > 0 && !bf16_mode) return hipErrorInvalidValue;
   dim3 grid(kAttnQB / 4, n_groups);
   if (bf16_mode)
-    hipLaunchKernelGGL(attn_merge_kernel<bf16>, grid, dim3(256), 0, s, groups, reqs, (const bf16 *)part_o, part_ml,
-                       (bf16 *)o, ldo, nq, nkv, hd, o_rows);
+    hipLaunchKernelGGL(attn_merge_kernel<bf16>, grid, dim3(256), 0, s, groups, (const bf16 *)part_o, part_ml,
+                       (bf16 *)o, ldo, nq, nkv, hd, o_rows, lse);
   else
-    hipLaunchKernelGGL(attn_merge_kernel<float>, grid, dim3(256), 0, s, groups, reqs, (const bf16 *)part_o, part_ml,
-                       (float *)o, ldo, nq, nkv, hd, 0);
+    hipLaunchKernelGGL(attn_merge_kernel<float>, grid, dim3(256), 0, s, groups, (const bf16 *)part_o, part_ml,
+                       (float *)o, ldo, nq, nkv, hd, 0, lse);
   return hipGetLastError();
 }
 

@@ -10,8 +10,6 @@
 
 namespace rosa {
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-
 // ------------------------------------------------------------------ to 4 bits and back
 // A block of 32 elements x: a = max |x|, e = the least integer with
 // a <= 7 2^e (a normal a = 1.m 2^E: E - 2 where 1.m <= 1.75, else E - 1),
@@ -60,19 +58,6 @@ __global__ void __launch_bounds__(256) kv_quantize_kernel(KvJobs jobs, int L, in
     reinterpret_cast<uint32_t *>(dst)[i] = c;
     if ((threadIdx.x & 3) == 0) scales[i >> 2] = finite ? (uint8_t)(e + 127) : 255;
   }
-}
-
-// A scale byte as the fp32 factor the conversions take; byte 255 turns every code to NaN.
-__device__ __forceinline__ float kv4_scale(uint8_t b) { return __uint_as_float((uint32_t)b << 23); }
-
-// 8 codes (4 bytes) as 8 bf16 values.
-__device__ __forceinline__ bf16x8 kv4_bf16x8(uint32_t c, float scale) {
-  const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0);
-  const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
-  const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2);
-  const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
-  return __builtin_bit_cast(bf16x8, make_uint4(__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1),
-                                               __builtin_bit_cast(uint32_t, v2), __builtin_bit_cast(uint32_t, v3)));
 }
 
 template <typename T>
@@ -376,7 +361,7 @@ __global__ void __launch_bounds__(256) kv_attention_rows_kernel(KvAttnArgs ka) {
     // row-major, or kb32
     if (g == 0) out[a.o_rows > 0 ? kb32_offset(a.o_rows, row, col + e) : row * a.ldo + col + e] = from_f32<T>(v * inv);
   }
-  if (ka.lse && lane == 0) ka.lse[row * a.nq + qg] = mx + logf(l);
+  if (a.lse && lane == 0) a.lse[row * a.nq + qg] = mx + logf(l);
 }
 
 template <int HD>

@@ -1,0 +1,571 @@
+// Ragged attention of action tokens over 4-bit prefix caches and their own bf16
+// keys and values (gfx950 MFMA), one layer.
+//
+// Work items, blocks and lists are those of the bf16 attention kernel: an
+// item is (request, KV head, up to 128 NG query rows, key range), four waves own
+// NG groups of 32 query rows each, S^T = K Q^T and O^T += V^T P^T with 32 x 32 MFMA tiles,
+// each lane one query column.  What differs is where K and V come from.
+//
+// K: the matrix cores read the codes themselves.  v_mfma_scale_f32_32x32x64_f8f6f4
+// takes a 4-bit operand whose lane holds 32 consecutive elements (16 bytes) of a row
+// and their scale byte: exactly a block of the cache.  The other operand, Q in bf16, is
+// split into three terms of 6 bits (e2m1's wider sibling e2m3: 4 significant bits
+// near the top of a block) on scales 2^e, 2^(e-4), 2^(e-9), e the least with
+// max|q| <= 7.5 2^e over 32 elements: q is then a multiple of 2^(e-12) and exact, unless it has
+// bits below that; so off by at most 2^(e-13) <= 2^-14.9 of the block's
+// largest magnitude, well below what rounding q to bf16 lost.  Three products with 6-bit operands at
+// 9.5 PFLOP/s (measured, 4 x 6 bit) cost 3/4 of one in bf16 (2.3 PFLOP/s), and no
+// instruction is spent on turning K to bf16.
+// V: its scales run along head_dim, across the product's summed index, so it is
+// turned to bf16 (exact): every thread converts one block of the next tile into
+// LDS, from where the transposed reads feed the MFMAs.
+// The request's own keys and values (bf16, at the end of the key range) run
+// through the same loop with bf16 products.
+#include <math.h>
+
+#include <type_traits>
+
+#include "rosa_device.h"
+#include "rosa_internal.h"
+
+namespace rosa {
+
+typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
+typedef __attribute__((ext_vector_type(6))) uint32_t u32x6;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+// Every wave's LDS accesses so far are done before any wave goes on.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// This wave's loads and copies have landed.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int HD, int NG>
+struct Kv4Tile {
+  static constexpr int ROWB = HD * 2, CPR = ROWB / 16;     // bf16 row: bytes, 16-byte chunks
+  static constexpr int TILEB = 32 * ROWB;                  // 32 bf16 rows
+  static constexpr int K4ROW = HD / 2, CK = HD / 32;       // code row: bytes, 16-byte chunks (blocks)
+  static constexpr int K4TILE = 32 * K4ROW;
+  static constexpr int NCH = HD >= 64 ? HD / 64 : 1;       // 64-wide products over head_dim
+  // LDS: V tiles (bf16) 2, own keys' K tiles (bf16) 2, K code tiles 3
+  static constexpr int AOFF = 2 * TILEB, KOFF = 4 * TILEB, RINGB = KOFF + 3 * K4TILE;
+  static constexpr int STGB = 4 * NG * 32 * 2 * HD;        // output staging
+  static constexpr int LDSB = RINGB > STGB ? RINGB : STGB;
+  // chunk swizzle of code rows: the 16 rows that a 16-lane group reads at one chunk fall in
+  // distinct 16-byte columns of the 256-byte bank row
+  static constexpr int SHIFT = K4ROW == 128 ? 1 : K4ROW == 64 ? 2 : K4ROW == 32 ? 3 : 4;
+  __device__ static int ksw(int row) { return (row >> SHIFT) & (CK - 1); }
+};
+
+// 32 consecutive query elements (16 words of bf16 pairs) as three 6-bit terms; returns
+// their scale bytes, first term's lowest.
+__device__ __forceinline__ uint32_t split_query(const bf16x8 (&q)[4], u32x6 (&t)[3]) {
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 u = __builtin_bit_cast(uint4, q[i]);
+    w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
+  }
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) a = max(a, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
+  const int E = (int)(a >> 23) - 127;
+  const int e = min(125, max(-115, (a & 0x7fffffu) <= 0x700000u ? E - 2 : E - 1));
+  bf16x32 r;
+  __builtin_memcpy(&r, w, sizeof r);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const float s = __uint_as_float((uint32_t)(e + 127 - (k == 0 ? 0 : k == 1 ? 4 : 9)) << 23);
+    t[k] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(r, s);
+    if (k == 2) break;
+    // what the term leaves: a multiple of the element's last bit and less than a step
+    // of the term, so exact in bf16
+    const bf16x32 b = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(t[k], s);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = (bf16)((float)r[i] - (float)b[i]);
+  }
+  // a NaN or an infinity in the block: every product with it is NaN
+  return a >= 0x7f800000u ? 0xffffffffu : (uint32_t)(e + 127) | (uint32_t)(e + 123) << 8 | (uint32_t)(e + 118) << 16;
+}
+
+template <int HD, int NG>
+__global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
+  using T = Kv4Tile<HD, NG>;
+  constexpr int NS = HD / 16, NT = HD / 32, CPR = T::CPR, ROWB = T::ROWB, TILEB = T::TILEB, CK = T::CK, NCH = T::NCH;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDSB];
+  const AttnArgs &a = ka.a;
+  if (a.ordered[blockIdx.x].nq <= 0) return;
+  const int G = a.nq / a.nkv;
+  const bf16 *qkv = reinterpret_cast<const bf16 *>(a.qkv);
+  const uint32_t lds0 = lds_u32(smem);
+  const float sl2 = 1.4426950408889634f / sqrtf((float)HD);   // log2(e) / sqrt(hd)
+
+  for (int e = blockIdx.x; e >= 0;) {
+  AttnItem it;
+  {
+    const uint32_t *src = reinterpret_cast<const uint32_t *>(a.ordered + e);
+    uint32_t w[sizeof(AttnItem) / 4];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(AttnItem) / 4); ++i) w[i] = __builtin_amdgcn_readfirstlane(src[i]);
+    __builtin_memcpy(&it, w, sizeof(AttnItem));
+  }
+  e = it.next;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));      // per-lane addresses are not kept across items
+  const int lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
+  const bool active = 32 * wave < it.nq;      // a wave without rows only helps with the copies
+
+  // Key range: prefix tiles [k0 + 32 t, + 32) with k0 = pe - 32 np (the first may
+  // reach below kbeg: masked), then own-key tiles likewise.
+  const int pe = min(it.kend, it.P), ab = max(it.kbeg, it.P);
+  const int np = pe > it.kbeg ? (pe - it.kbeg + 31) >> 5 : 0, k0 = pe - 32 * np;
+  const int na = it.kend > ab ? (it.kend - ab + 31) >> 5 : 0, a0 = it.kend - 32 * na;
+
+  const size_t rowb = (size_t)a.nkv * T::K4ROW, srow = (size_t)a.nkv * CK;
+  const size_t r0 = (size_t)a.layer * it.P * a.nkv + it.kvh, codes = kv4_code_bytes(ka.L, it.P, a.nkv, HD);
+  const uint8_t *kc = reinterpret_cast<const uint8_t *>(it.pk) + r0 * T::K4ROW;
+  const uint8_t *vc = reinterpret_cast<const uint8_t *>(it.pv) + r0 * T::K4ROW;
+  const uint8_t *ks = reinterpret_cast<const uint8_t *>(it.pk) + codes + r0 * CK;
+  const uint8_t *vs = reinterpret_cast<const uint8_t *>(it.pv) + codes + r0 * CK;
+
+  // ---- copies
+  // K codes of prefix tile t into ring stage t % 3: 1 KB a wave
+  auto copy_k4 = [&](int t) __attribute__((always_inline)) {
+    if (t >= np) return;
+    if (1024 * wave >= T::K4TILE || (T::K4TILE < 1024 && lane >= 32)) return;
+    const int p = wave * 64 + lane, row = p / CK, c = (p % CK) ^ T::ksw(row);
+    const int key = max(k0 + 32 * t + row, it.kbeg);
+    dma_1k(kc + (size_t)key * rowb + c * 16, lds0 + T::KOFF + (uint32_t)(t % 3) * T::K4TILE + wave * 1024);
+  };
+  // own keys: one bf16 tile (K or V columns) into LDS at dst
+  auto copy_own = [&](int u, int col, uint32_t dst) __attribute__((always_inline)) {
+    constexpr int UNITS = TILEB / 1024, RPU = 1024 / ROWB;
+#pragma unroll
+    for (int j = 0; j < (UNITS + 3) / 4; ++j) {
+      if (4 * j + wave >= UNITS) continue;
+      const int row = (4 * j + wave) * RPU + lane / CPR, c = (lane % CPR) ^ at::swz(row, CPR);
+      const int key = max(a0 + 32 * u + row, ab) - it.P;
+      dma_1k(qkv + (size_t)(it.tok_off + key) * a.ldqkv + col + c * 8, dst + (4 * j + wave) * 1024);
+    }
+  };
+  const int kcol = (a.nq + it.kvh) * HD, vcol = (a.nq + a.nkv + it.kvh) * HD;
+  auto vstage = [&](int t) { return lds0 + (uint32_t)((t & 1) * TILEB); };
+  auto astage = [&](int t) { return lds0 + (uint32_t)(T::AOFF + (t & 1) * TILEB); };
+
+  // V: this thread's block (vrow, vblk) of a tile, held from its load to its conversion one step
+  // later.  Lanes are dealt so that the 16 of a group write distinct 16-byte columns.
+  int vrow, vblk;
+  if constexpr (HD == 256) {
+    vblk = (lane & 3) | ((lane >> 2) & 4);
+    vrow = (((lane >> 2) & 3) << 2) | (lane >> 5) | ((wave & 1) << 1) | ((wave >> 1) << 4);
+  } else if constexpr (HD == 128) {
+    vblk = lane & 3;
+    vrow = (((lane >> 2) & 3) << 2) | (lane >> 4) | ((wave & 1) << 4);
+  } else {
+    vblk = tid % CK;
+    vrow = (tid / CK) & 31;
+  }
+  uint4 vreg = make_uint4(0, 0, 0, 0);
+  uint32_t vscale = 0;
+  auto load_v = [&](int t) __attribute__((always_inline)) {
+    if (t >= np || tid >= HD) return;
+    const size_t key = (size_t)max(k0 + 32 * t + vrow, it.kbeg);
+    vreg = *reinterpret_cast<const uint4 *>(vc + key * rowb + vblk * 16);
+    vscale = vs[key * srow + vblk];
+  };
+  auto write_v = [&](int t) __attribute__((always_inline)) {
+    if (tid >= HD) return;
+    const float s = kv4_scale((uint8_t)vscale);
+    const uint32_t w[4] = {vreg.x, vreg.y, vreg.z, vreg.w};
+    uint8_t *dst = smem + (t & 1) * TILEB + vrow * ROWB;
+    const int sw = at::swz(vrow, CPR);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<bf16x8 *>(dst + (((4 * vblk + i) ^ sw) << 4)) = kv4_bf16x8(w[i], s);
+  };
+  // K scale bytes of this lane's row (lane & 31) of tile t, byte c for its block of product c
+  auto load_kscale = [&](int t) __attribute__((always_inline)) -> uint32_t {
+    const size_t key = (size_t)max(k0 + 32 * min(t, np - 1) + (lane & 31), it.kbeg);
+    const uint8_t *p = ks + key * srow;
+    if constexpr (CK == 8) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(p);
+      return __builtin_amdgcn_perm(v.y, v.x, half ? 0x07050301u : 0x06040200u);
+    } else if constexpr (CK == 4) {
+      const uint32_t v = *reinterpret_cast<const uint32_t *>(p);
+      return __builtin_amdgcn_perm(0u, v, half ? 0x03030301u : 0x02020200u);
+    } else {
+      return p[CK == 2 ? half : 0];
+    }
+  };
+
+  // ---- LDS operand addresses
+  const int krow = lane & 31;
+  // code chunk 2 c + half of the lane's row: base ^ 32 c (rows and stages are multiples of the
+  // swizzled bits' span)
+  const uint32_t k4base = lds0 + T::KOFF + krow * T::K4ROW + (CK == 1 ? 0 : ((half ^ T::ksw(krow)) << 4));
+  // own-key K chunk HD >= 64: 8 c + 4 half + j (a lane's elements 32 consecutive, as in the codes),
+  // HD 32: 2 j + half
+  const uint32_t abase = (uint32_t)(krow * ROWB + (((HD == 32 ? half : 4 * half) ^ at::swz(krow, CPR)) << 4));
+  const int src16 = lane & 15, g16 = (lane >> 4) & 1;
+  uint32_t vbase[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = half * 4 + (src16 >> 2) + 8 * h;
+    const int sw = at::swz(r, CPR);
+    const int cl = (2 * g16 + ((src16 >> 1) & 1)) ^ (sw & 3);
+    vbase[h] = (uint32_t)(r * ROWB + 16 * cl + 8 * (src16 & 1)) ^ ((uint32_t)(sw >> 2) << 6);
+  }
+
+  // ---- queries
+  const bf16 *qp[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const int loc = 32 * (wave + 4 * g) + (lane & 31);
+    const int qrow = it.q0 + (loc < it.nq ? loc : 0);   // rows past the item's: its first (never stored)
+    qp[g] = qkv + (size_t)(it.tok_off + qrow / G) * a.ldqkv + (size_t)(it.kvh * G + qrow % G) * HD;
+  }
+
+  f32x16 o[NG][NT];
+  float m_ref[NG], l_run[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    m_ref[g] = -INFINITY;
+    l_run[g] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[g][n][r] = 0.f;
+  }
+
+  // Softmax of one tile of scores (register r: key (r/4)*8 + 4 half + r%4) into P^T.
+  // Weights are 2^((s - m_ref) sl2) against a reference that is the first tile's maximum and
+  // moves (with O and the sum rescaled) only when a score exceeds it by 2^32 in weight: weights
+  // and sums stay far from overflow, and the accumulators are left alone nearly always.
+  // lo: keys of the tile below this index are masked.
+  auto softmax = [&](f32x16 (&s)[NG], bf16x8 (&pp)[NG][2], int lo) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if (lo > 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if ((r >> 2) * 8 + half * 4 + (r & 3) < lo) s[g][r] = -INFINITY;
+      }
+      float tmax = fmaxf(s[g][0], s[g][1]);
+#pragma unroll
+      for (int r = 2; r < 16; ++r) tmax = fmaxf(tmax, s[g][r]);
+      if (__ballot((tmax - m_ref[g]) * sl2 > 32.0f)) {    // also every first tile (m_ref = -inf)
+        const float tm = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+        const bool up = (tm - m_ref[g]) * sl2 > 32.0f;    // the halves of a query agree
+        const float f = up ? __builtin_amdgcn_exp2f((m_ref[g] - tm) * sl2) : 1.0f;
+        if (up) m_ref[g] = tm;
+        l_run[g] *= f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[g][n][r] *= f;
+      }
+      const float mb = m_ref[g] == -INFINITY ? 0.f : -m_ref[g] * sl2;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[g][r] = __builtin_amdgcn_exp2f(fmaf(s[g][r], sl2, mb));
+      float ps = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+          bf16x2 p2;
+          p2[0] = (bf16)s[g][8 * h + 2 * q];
+          p2[1] = (bf16)s[g][8 * h + 2 * q + 1];
+          ps += s[g][8 * h + 2 * q] + s[g][8 * h + 2 * q + 1];
+          w[q] = __builtin_bit_cast(uint32_t, p2);
+        }
+        pp[g][h] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+      }
+      l_run[g] += ps;
+    }
+  };
+  // O^T += V^T P^T over the V tile at vst
+  auto pv_acc = [&](uint32_t vst, const bf16x8 (&pp)[NG][2]) __attribute__((always_inline)) {
+    const uint32_t v0 = vst + vbase[0], v1 = vst + vbase[1];
+    auto vfrag = [&](int j) __attribute__((always_inline)) -> bf16x8 {
+      const int kk = j / NT, n = j % NT, c = (n / 4) * 256 + kk * 16 * ROWB;
+      const uint32_t x = (uint32_t)(64 * (n % 4));
+      return lds_tr_pair(lds_ptr(v0 ^ x) + c, lds_ptr(v1 ^ x) + c);
+    };
+    constexpr int NJ = 2 * NT;
+    bf16x8 fr[3];
+    fr[0] = vfrag(0);
+    fr[1] = vfrag(1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      if (j + 2 < NJ) fr[(j + 2) % 3] = vfrag(j + 2);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) o[g][j % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[j % 3], pp[g][j / NT], o[g][j % NT], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // ---- prologue: the first tiles' copies, then the queries
+  if (np > 0) {
+    copy_k4(0);
+    copy_k4(1);
+    load_v(0);
+  } else {
+    copy_own(0, kcol, astage(0));
+    copy_own(0, vcol, vstage(0));
+  }
+  if (np > 0) {
+    u32x6 q6[NG][NCH][3];
+    uint32_t qs[NG][NCH];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        bf16x8 q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          q[j] = *reinterpret_cast<const bf16x8 *>(qp[g] + 64 * c + (HD == 32 ? 0 : 32 * half) + 8 * j);
+          if (HD == 32 && half) q[j] = bf16x8{};        // a product is 64 wide
+        }
+        qs[g][c] = split_query(q, q6[g][c]);
+      }
+    wait_loads();
+    write_v(0);
+    load_v(1);
+    uint32_t ksc = load_kscale(0);
+    for (int t = 0; t < np; ++t) {
+      lds_barrier();                        // tile t is in LDS; every wave is done with tile t - 1
+      const uint32_t ksn = load_kscale(t + 1);
+      f32x16 s[NG];
+      bf16x8 pp[NG][2];
+      if (active) {
+        const uint32_t kb = k4base + (uint32_t)(t % 3) * T::K4TILE;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+          i32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(lds_ptr(kb ^ (uint32_t)(32 * c)));
+          if (HD == 32 && half) k = i32x4{};
+          const i32x8 kf = {k[0], k[1], k[2], k[3], 0, 0, 0, 0};
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            auto term = [&](auto kk) __attribute__((always_inline)) {
+              constexpr int K = decltype(kk)::value;
+              const u32x6 &x = q6[g][c][K];
+              const i32x8 qf = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+              const f32x16 acc = c == 0 && K == 0 ? f32x16{} : s[g];
+              if (c == 0) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 0, ksc, K, qs[g][c]);
+              if (c == 1) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 1, ksc, K, qs[g][c]);
+              if (c == 2) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 2, ksc, K, qs[g][c]);
+              if (c == 3) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 3, ksc, K, qs[g][c]);
+            };
+            term(std::integral_constant<int, 0>{});
+            term(std::integral_constant<int, 1>{});
+            term(std::integral_constant<int, 2>{});
+          }
+        }
+        softmax(s, pp, t == 0 ? it.kbeg - k0 : 0);
+      }
+      // V of tile t + 1 to the other stage; then the loads for the tiles behind it.
+      // K codes t + 1 landed with V (issued before it).
+      wait_loads();
+      if (t + 1 < np) {
+        write_v(t + 1);
+        copy_k4(t + 2);
+        load_v(t + 2);
+      } else if (na > 0) {
+        copy_own(0, kcol, astage(t + 1));
+        copy_own(0, vcol, vstage(t + 1));
+      }
+      ksc = ksn;
+      __builtin_amdgcn_sched_barrier(0);
+      if (active) pv_acc(vstage(t), pp);
+    }
+  }
+  // ---- the request's own keys
+  if (na > 0) {
+    bf16x8 qf[NG][NS];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        // fragment i: elements 64 (i / 4) + 32 half + 8 (i % 4) (HD 32: 16 i + 8 half)
+        const int at = HD == 32 ? 16 * i + 8 * half : 64 * (i / 4) + 32 * half + 8 * (i % 4);
+        qf[g][i] = *reinterpret_cast<const bf16x8 *>(qp[g] + at);
+      }
+    for (int u = 0; u < na; ++u) {
+      const int t = np + u;
+      wait_loads();
+      lds_barrier();
+      f32x16 s[NG];
+      bf16x8 pp[NG][2];
+      if (active) {
+        const uint32_t ab0 = astage(t) + abase;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const uint32_t x = (uint32_t)((HD == 32 ? 2 * i : 8 * (i / 4) + i % 4) << 4);
+          const bf16x8 kf = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds_ptr(ab0 ^ x));
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[g][i], i == 0 ? f32x16{} : s[g], 0, 0, 0);
+        }
+        softmax(s, pp, u == 0 ? ab - a0 : 0);
+      }
+      if (u + 1 < na) {
+        copy_own(u + 1, kcol, astage(t + 1));
+        copy_own(u + 1, vcol, vstage(t + 1));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (active) pv_acc(vstage(t), pp);
+    }
+  }
+  wait_loads();
+  lds_barrier();                          // every wave is done with the rings
+
+  // ---- results.  Lane: query (lane & 31) of the group; register r of tile n: element
+  // 32 n + (r/4)*8 + 4 half + r%4.
+  constexpr int CPRO = HD / 8;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const float l = l_run[g] + __shfl_xor(l_run[g], 32, 64);
+    const int loc = 32 * (wave + 4 * g) + (lane & 31);
+    if (loc >= it.nq) continue;
+    const float m2 = m_ref[g] * sl2;                      // log2 units
+    if (it.slot >= 0) {
+      const size_t pr = (size_t)it.slot * kAttnQB + loc;
+      float *po = reinterpret_cast<float *>(a.part_o) + pr * HD + 4 * half;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4 *>(po + 32 * n + 8 * q) =
+              make_float4(o[g][n][4 * q], o[g][n][4 * q + 1], o[g][n][4 * q + 2], o[g][n][4 * q + 3]);
+      if (half == 0) *reinterpret_cast<float2 *>(a.part_ml + pr * 2) = make_float2(m2, l);
+      continue;
+    }
+    const int qrow = it.q0 + loc;
+    if (a.lse && half == 0)
+      a.lse[(size_t)(it.tok_off + qrow / G) * a.nq + it.kvh * G + qrow % G] = (m2 + log2f(l)) * 0.6931471805599453f;
+    // through LDS, so that whole 16-byte chunks of rows go out side by side
+    const float inv = 1.0f / l;
+    uint8_t *stg = smem + (wave * NG + g) * (32 * 2 * HD);
+    const int q = lane & 31;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        bf16x4 v;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = (bf16)(o[g][n][rg * 4 + x] * inv);
+        const int c = (4 * n + rg) ^ (q & (CPRO - 1));
+        *reinterpret_cast<bf16x4 *>(stg + q * 2 * HD + c * 16 + half * 8) = v;
+      }
+  }
+  if (it.slot < 0) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's staging writes are done
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int base = 32 * (wave + 4 * g);
+      if (base >= it.nq) continue;
+      const uint8_t *stg = smem + (wave * NG + g) * (32 * 2 * HD);
+      constexpr int RPI = 64 / CPRO;
+#pragma unroll
+      for (int i = 0; i < 32 / RPI; ++i) {
+        const int r = i * RPI + lane / CPRO, c = lane % CPRO;
+        if (base + r < it.nq) {
+          const uint4 v = *reinterpret_cast<const uint4 *>(stg + r * 2 * HD + ((c ^ (r & (CPRO - 1))) * 16));
+          const int qrow = it.q0 + base + r;
+          const size_t orow = (size_t)(it.tok_off + qrow / G), ocol = (size_t)(it.kvh * G + qrow % G) * HD + c * 8;
+          bf16 *dst = reinterpret_cast<bf16 *>(a.o) + (a.o_rows > 0 ? kb32_offset(a.o_rows, orow, ocol) : orow * a.ldo + ocol);
+          *reinterpret_cast<uint4 *>(dst) = v;
+        }
+      }
+    }
+  }
+  lds_barrier();                          // the staging reads are done before the next item's copies
+  }
+}
+
+hipError_t launch_kv4_attention(const KvAttnArgs &ka, hipStream_t s) {
+  const AttnArgs &a = ka.a;
+  if (a.n_blocks <= 0) return hipSuccess;
+  dim3 grid(a.n_blocks);
+  switch (a.hd) {
+    case 32: hipLaunchKernelGGL((kv4_attention_kernel<32, attn_groups_per_wave(32)>), grid, dim3(256), 0, s, ka); break;
+    case 64: hipLaunchKernelGGL((kv4_attention_kernel<64, attn_groups_per_wave(64)>), grid, dim3(256), 0, s, ka); break;
+    case 128: hipLaunchKernelGGL((kv4_attention_kernel<128, attn_groups_per_wave(128)>), grid, dim3(256), 0, s, ka); break;
+    case 256: hipLaunchKernelGGL((kv4_attention_kernel<256, attn_groups_per_wave(256)>), grid, dim3(256), 0, s, ka); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ joining split items
+// One wave per query row: o = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c, slots in
+// order.  Lane holds head-dim elements 4 lane ..
+__global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restrict__ groups, KvAttnArgs ka) {
+  const AttnArgs &a = ka.a;
+  const AttnGroup gr = groups[blockIdx.y];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int qloc = blockIdx.x * 4 + wave, G = a.nq / a.nkv, hd = a.hd;
+  if (qloc >= gr.nq) return;
+  const bool on = 4 * lane < hd;
+  const float *po = reinterpret_cast<const float *>(a.part_o);
+  const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
+  // a lane's share of the slots' maxima and sums
+  float mx = -INFINITY;
+  for (int c = lane; c < gr.n; c += 64) mx = fmaxf(mx, ml[(size_t)(gr.first_slot + c) * kAttnQB + qloc].x);
+  mx = wave_max(mx);
+  constexpr int CH = 8;
+  float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int c0 = 0; c0 < gr.n; c0 += CH) {
+    float2 p[CH];
+    float4 v[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const bool live = c0 + c < gr.n;
+      const size_t r = (size_t)(gr.first_slot + (live ? c0 + c : 0)) * kAttnQB + qloc;
+      p[c] = live ? ml[r] : make_float2(-INFINITY, 0.f);
+      v[c] = live && on ? *reinterpret_cast<const float4 *>(po + r * hd + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const float w = exp2f(p[c].x - mx);
+      if (c0 + c >= gr.n) break;
+      L += w * p[c].y;
+      acc[0] += w * v[c].x; acc[1] += w * v[c].y; acc[2] += w * v[c].z; acc[3] += w * v[c].w;
+    }
+  }
+  const int qrow = gr.q0 + qloc;
+  const size_t orow = (size_t)gr.tok_off + qrow / G;
+  const int qg = gr.kvh * G + qrow % G;
+  if (a.lse && lane == 0) a.lse[orow * a.nq + qg] = (mx + log2f(L)) * 0.6931471805599453f;
+  if (!on) return;
+  const float inv = 1.0f / L;
+  const size_t col = (size_t)qg * hd + 4 * lane;
+  bf16x4 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = (bf16)(acc[j] * inv);
+  *reinterpret_cast<bf16x4 *>(reinterpret_cast<bf16 *>(a.o) + (a.o_rows > 0 ? kb32_offset(a.o_rows, orow, col) : orow * a.ldo + col)) = r;
+}
+
+hipError_t launch_kv4_merge(const AttnGroup *groups, int n_groups, const KvAttnArgs &a, hipStream_t s) {
+  if (n_groups <= 0) return hipSuccess;
+  hipLaunchKernelGGL(kv4_merge_kernel, dim3(kAttnQB / 4, n_groups), dim3(256), 0, s, groups, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_attention(const KvAttnArgs &ka, const AttnGroup *groups, int n_groups, bool bf16_mode, hipStream_t s) {
+  if (!bf16_mode) return launch_kv_attention_rows(ka, false, s);
+  const AttnArgs &a = ka.a;
+  if (ka.fp4) {
+    const hipError_t e = launch_kv4_attention(ka, s);
+    return e != hipSuccess ? e : launch_kv4_merge(groups, n_groups, ka, s);
+  }
+  const hipError_t e = launch_attention(a, true, s);
+  return e != hipSuccess ? e
+                         : launch_attn_merge(groups, n_groups, a.part_o, a.part_ml, a.o, a.ldo, a.nq, a.nkv, a.hd, true, s,
+                                             a.o_rows, a.lse);
+}
+
+}  // namespace rosa

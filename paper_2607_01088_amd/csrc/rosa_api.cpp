@@ -525,7 +525,7 @@ rosa_status build_plan(const rosa_model_config *cfg, const rosa_capacity *cap, c
           const int q0 = 32 * (qb * ngrp / nqb);
           const int nq = std::min(R, 32 * ((qb + 1) * ngrp / nqb)) - q0;
           if (nsplit > 1) {
-            AttnGroup gr{i, kvh, q0, nq, p.slots, nsplit, 0, 0};
+            AttnGroup gr{i, kvh, q0, nq, p.slots, nsplit, p.tok_off[i], 0};
             S.groups.push_back(gr);
           }
           for (int c = 0; c < nsplit; ++c) {
@@ -768,9 +768,12 @@ hipError_t run_attention(rosa_batch *b, const Plan &p, const Plan::Lane &ln, int
   a.part_o = b->part_o; a.part_ml = b->part_ml;
   if (kv && !kv->plain()) {
     KvAttnArgs ka{};
-    ka.a = a; ka.a.items = items + it_lo;
-    ka.L = D.L; ka.fp4 = kv->fp4; ka.lse = kv->gather && v == 0 ? b->lse : nullptr;
-    hipError_t e = timed(b, kcAttention, [&] { return launch_kv_attention_rows(ka, b->bf16, st); });
+    ka.a = a;
+    ka.a.lse = kv->gather && v == 0 ? b->lse : nullptr;
+    ka.L = D.L; ka.fp4 = kv->fp4;
+    hipError_t e = timed(b, kcAttention, [&] {
+      return launch_kv_attention(ka, groups + gr_lo, gr_hi - gr_lo, b->bf16, st);
+    });
     const int m_lo = kv->gather && r0 > 0 ? kv->upto[r0 - 1] : 0, m_hi = kv->gather ? kv->upto[r0 + n_act - 1] : 0;
     if (e != hipSuccess || v != 0 || m_hi == m_lo) return e;
     KvMassArgs ma{};
@@ -785,7 +788,7 @@ hipError_t run_attention(rosa_batch *b, const Plan &p, const Plan::Lane &ln, int
   hipError_t e = timed(b, kcAttention, [&] { return launch_attention(a, b->bf16, st); });
   if (e == hipSuccess && gr_hi > gr_lo)
     e = timed(b, kcMerge, [&] {
-      return launch_attn_merge(groups + gr_lo, gr_hi - gr_lo, reqs, b->part_o, b->part_ml, o, D.o_dim, D.nq, D.nkv,
+      return launch_attn_merge(groups + gr_lo, gr_hi - gr_lo, b->part_o, b->part_ml, o, D.o_dim, D.nq, D.nkv,
                                D.hd, b->bf16, st, o_rows);
     });
   return e;
@@ -1078,7 +1081,7 @@ static rosa_status generate(rosa_batch *b, const rosa_request *reqs, int32_t n, 
     std::string err;
     // Lanes only without per-kernel profiling (its events live on one stream).
     const int lanes = b->prof ? 1 : call_lanes(b->cap, reqs, n, max_steps, b->lanes);
-    rosa_status st = build_plan(&b->cfg, &b->cap, reqs, n, true, b->bf16 && kv.plain(), lanes, p, err, max_steps);
+    rosa_status st = build_plan(&b->cfg, &b->cap, reqs, n, true, b->bf16, lanes, p, err, max_steps);
     if (st != ROSA_OK) return fail(b, st, err);
     if (n == 0) return ROSA_OK;
     if (!kv.plain()) {
@@ -1554,7 +1557,7 @@ rosa_status rosa_attention_noalloc(const rosa_model_config *cfg, const rosa_requ
     e = launch_attention(a, bf16, stream);
     if (e == hipSuccess && !S.groups.empty())
       e = launch_attn_merge(reinterpret_cast<const AttnGroup *>(sp + off_groups), (int)S.groups.size(),
-                            a.reqs, a.part_o, a.part_ml, o, D.o_dim, D.nq, D.nkv, D.hd, bf16, stream);
+                            a.part_o, a.part_ml, o, D.o_dim, D.nq, D.nkv, D.hd, bf16, stream);
     return e == hipSuccess ? ROSA_OK : device_fail(nullptr, e, "attention launch");
   } catch (const std::bad_alloc &) {
     return fail(nullptr, ROSA_E_NOMEM, "host allocation failed");

@@ -78,4 +78,40 @@ __device__ __forceinline__ float gelu_tanh_f(float x) {
   return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
+namespace at {
+constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+// Chunk swizzle of LDS rows: 16-byte chunk c of row r is stored at c ^ swz(r),
+// swz(r) = the two 2-bit halves of r % 16 swapped.  The 16 consecutive rows
+// that one 16-lane group reads at one chunk (K operand), and the 4 rows x 4
+// chunks that the transpose reads of a 32-lane half touch (V operand), then
+// fall in distinct bank groups.
+__device__ __forceinline__ int swz(int r, int cpr) { return (((r & 3) << 2) | ((r >> 2) & 3)) & (cpr - 1); }
+}  // namespace at
+
+typedef __attribute__((address_space(3))) const uint8_t lds_u8;
+__device__ __forceinline__ const lds_u8 *lds_ptr(uint32_t a) { return (const lds_u8 *)(size_t)a; }
+__device__ __forceinline__ bf16x8 lds_tr_pair(const lds_u8 *p0, const lds_u8 *p1) {
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p0));
+  const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p1));
+  const uint2 u0 = __builtin_bit_cast(uint2, v0);
+  const uint2 u1 = __builtin_bit_cast(uint2, v1);
+  return __builtin_bit_cast(bf16x8, make_uint4(u0.x, u0.y, u1.x, u1.y));
+}
+
+// A 4-bit cache's scale byte as the fp32 factor the conversions take; byte 255 turns every
+// code to NaN.
+__device__ __forceinline__ float kv4_scale(uint8_t b) { return __uint_as_float((uint32_t)b << 23); }
+
+// 8 codes (4 bytes) as 8 bf16 values.
+__device__ __forceinline__ bf16x8 kv4_bf16x8(uint32_t c, float scale) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  const bf16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0);
+  const bf16x2 v1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+  const bf16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2);
+  const bf16x2 v3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+  return __builtin_bit_cast(bf16x8, make_uint4(__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1),
+                                               __builtin_bit_cast(uint32_t, v2), __builtin_bit_cast(uint32_t, v3)));
+}
+
 }  // namespace rosa

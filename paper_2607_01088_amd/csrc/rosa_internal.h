@@ -48,7 +48,7 @@ static_assert(sizeof(AttnItem) == 64, "AttnItem is 64 bytes");
 // A query block whose keys were split over n items (partial slots first_slot
 // .. first_slot + n - 1).
 struct AttnGroup {
-  int32_t req, kvh, q0, nq, first_slot, n, pad0, pad1;
+  int32_t req, kvh, q0, nq, first_slot, n, tok_off, pad1;
 };
 static_assert(sizeof(AttnGroup) == 32, "AttnGroup is 32 bytes");
 
@@ -243,6 +243,9 @@ struct AttnArgs {
   // 1: every item's causal_b masks keys per query token (the prefix
   // producer's causal segments); such items are never key-split.
   int causal;
+  // Non-NULL: the rows' log-sum-exp, [stacked row][nq] fp32 (bf16 kernel, not causal; of
+  // split items the merge writes it).
+  float *lse;
 };
 hipError_t launch_attention(const AttnArgs &a, bool bf16, hipStream_t s);
 // Host: XCD-balanced item lists of persistent blocks for the items of the
@@ -268,9 +271,8 @@ inline hipError_t upload_gemm_weights(void *dst, const float *src, int L, int K,
 // nq = 0), each with its `next` link, written to dst.
 void attn_order_items(const std::vector<AttnItem> &items, const int32_t *order, const int32_t *next, size_t n,
                       AttnItem *dst);
-hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const ReqDesc *reqs,
-                             const void *part_o, const float *part_ml, void *o, int ldo, int nq,
-                             int nkv, int hd, bool bf16, hipStream_t s, int o_rows = 0);
+hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const void *part_o, const float *part_ml, void *o, int ldo, int nq,
+                             int nkv, int hd, bool bf16, hipStream_t s, int o_rows = 0, float *lse = nullptr);
 
 // ------------------------------------------------------------------ 4-bit caches and eviction
 // One 4-bit cache (K or V of one request): codes [L][P][nkv][hd / 2] bytes, then
@@ -302,16 +304,22 @@ struct KvEvictJobs { KvEvictJob j[kKvEvictJobs]; };
 // fp4: 4-bit caches, else rows of hd elements of esz bytes.
 hipError_t launch_kv_evict(const KvEvictJobs &jobs, int n, int L, int nkv, int hd, int esz, bool fp4, hipStream_t s);
 
-// Attention over caches in either format, fp32 sums throughout (`bf16`: the
-// type of qkv, o and model-type caches); items are not split over keys.
-// lse: [stacked row][nq], or NULL.
+// Attention over caches in either format; a.lse as in AttnArgs.
 struct KvAttnArgs {
   AttnArgs a;
   int L;                 // layers of the caches
   bool fp4;
-  float *lse;
 };
+// One wave per query row, fp32 throughout (`bf16`: the type of qkv, o and model-type
+// caches): the fp32 mode's kernel.  Items are not split over keys.
 hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16, hipStream_t s);
+// bf16 mode, 4-bit caches: the launch lists of a (ordered, n_blocks); partial results
+// of split items as part_o [slot][kAttnQB][hd] fp32 and part_ml.
+hipError_t launch_kv4_attention(const KvAttnArgs &a, hipStream_t s);
+hipError_t launch_kv4_merge(const AttnGroup *groups, int n_groups, const KvAttnArgs &a, hipStream_t s);
+// The attention of a's items with whatever kernels its format and mode take, and the join of
+// the split ones.
+hipError_t launch_kv_attention(const KvAttnArgs &a, const AttnGroup *groups, int n_groups, bool bf16, hipStream_t s);
 
 // Keys [k0, k0 + nk) of one KV head of one request, whose attention weight
 // is summed over the request's H action tokens (nk <= kMassKeys).

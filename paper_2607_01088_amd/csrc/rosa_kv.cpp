@@ -285,7 +285,7 @@ rosa_status rosa_kv_create(const rosa_model_config *cfg, const rosa_capacity *ca
     h->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassKeys) + (size_t)cap->max_requests);
     auto align = [](size_t v) { return (v + 255) / 256 * 256; };
     h->off_items = 0;
-    h->off_groups = align(h->off_items + h->max_items * sizeof(AttnItem));
+    h->off_groups = align(h->off_items + (h->bf16 ? 0 : h->max_items) * sizeof(AttnItem));
     h->off_lists = align(h->off_groups + h->max_groups * sizeof(AttnGroup));
     h->off_mass = align(h->off_lists + (h->bf16 ? h->max_lists : 0) * sizeof(AttnItem));
     h->plan_bytes = align(h->off_mass + h->max_mass * sizeof(MassItem));
@@ -333,7 +333,7 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     }
     Plan p;
     std::string err;
-    const rosa_status st = build_plan(&h->cfg, &h->cap, rq.data(), n, false, false, 1, p, err);
+    const rosa_status st = build_plan(&h->cfg, &h->cap, rq.data(), n, false, h->bf16, 1, p, err);
     if (st != ROSA_OK) return fail(h, st, err);
     for (int i = 0; i < n; ++i) {
       if (!aligned(rq[i].prefix_k, 16) || !aligned(rq[i].prefix_v, 16))
@@ -369,7 +369,7 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     all.insert(all.end(), S1.items.begin(), S1.items.end());
     if (h->bf16)
       attn_order_items(all, p.attn_lists.data(), p.attn_next.data(), p.attn_lists.size(), (AttnItem *)(hp + h->off_lists));
-    if (!all.empty())
+    else if (!all.empty())
       std::memcpy(hp + h->off_items, all.data(), all.size() * sizeof(AttnItem));
     if (!S0.groups.empty()) std::memcpy(hp + h->off_groups, S0.groups.data(), S0.groups.size() * sizeof(AttnGroup));
     if (!S1.groups.empty())
@@ -377,7 +377,7 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     if (!mi.empty()) std::memcpy(hp + h->off_mass, mi.data(), mi.size() * sizeof(MassItem));
     // only the parts in use are copied
     struct Part { size_t off, bytes; } parts[4] = {
-        {h->off_items, all.size() * sizeof(AttnItem)}, {h->off_groups, n_groups * sizeof(AttnGroup)},
+        {h->off_items, h->bf16 ? 0 : all.size() * sizeof(AttnItem)}, {h->off_groups, n_groups * sizeof(AttnGroup)},
         {h->off_lists, h->bf16 ? p.attn_lists.size() * sizeof(AttnItem) : 0}, {h->off_mass, mi.size() * sizeof(MassItem)}};
     for (const Part &q : parts)
       if (e == hipSuccess && q.bytes)
@@ -426,14 +426,16 @@ rosa_status rosa_kv_attention(rosa_kv *h, int32_t layer, const void *qkv, void *
     AttnArgs &a = ka.a;
     a.ordered = (const AttnItem *)(h->d_plan + h->off_lists) + S.list_at;
     a.n_blocks = S.blocks;
-    a.items = (const AttnItem *)(h->d_plan + h->off_items) + S.item_base;
+    a.items = h->bf16 ? a.ordered : (const AttnItem *)(h->d_plan + h->off_items) + S.item_base;
     a.n_items = S.items;
     a.layer = layer;
     a.qkv = qkv; a.ldqkv = D.qkv_dim; a.o = o; a.ldo = D.o_dim;
     a.nq = D.nq; a.nkv = D.nkv; a.hd = D.hd;
     a.part_o = h->part_o; a.part_ml = h->part_ml;
-    ka.L = D.L; ka.fp4 = h->fp4; ka.lse = lse;
-    if (e == hipSuccess) e = launch_kv_attention_rows(ka, h->bf16, h->stream);
+    a.lse = lse;
+    ka.L = D.L; ka.fp4 = h->fp4;
+    if (e == hipSuccess)
+      e = launch_kv_attention(ka, (const AttnGroup *)(h->d_plan + h->off_groups) + S.group_base, S.groups, h->bf16, h->stream);
     return e == hipSuccess ? ROSA_OK : device_fail(h, e, "attention");
   } catch (...) {
     return fail(h, ROSA_E_DEVICE, "unexpected exception");

@@ -267,7 +267,7 @@ rosa_status build_prefill_plan(const rosa_prefill *h, const rosa_prefix_job *job
       for (int qb = 0; qb < nqb; ++qb) {
         const int q0 = 32 * (qb * ngrp / nqb);
         const int nq = std::min(R, 32 * ((qb + 1) * ngrp / nqb)) - q0;
-        if (nsplit > 1) p.groups.push_back(AttnGroup{i, kvh, q0, nq, slots, nsplit, 0, 0});
+        if (nsplit > 1) p.groups.push_back(AttnGroup{i, kvh, q0, nq, slots, nsplit, (int32_t)p.jobs[i].tok_off, 0});
         for (int c = 0; c < nsplit; ++c) {
           AttnItem it{};
           it.pk = h->qkv; it.pv = h->qkv; it.P = 0; it.tok_off = (int32_t)p.jobs[i].tok_off;
@@ -514,8 +514,8 @@ rosa_status rosa_prefill_run(rosa_prefill *h, const rosa_prefix_job *jobs, int32
       e = ptimed(h, pcAttention, [&] { return launch_attention(a, h->bf16, s); });
       if (e == hipSuccess && !p.groups.empty())
         e = ptimed(h, pcMerge, [&] {
-          return launch_attn_merge(d_groups, (int)p.groups.size(), d_reqs, h->part_o, h->part_ml, h->o, h->o_dim,
-                                   h->nq, h->nkv, h->hd, h->bf16, s, h->kb_rows);
+          return launch_attn_merge(d_groups, (int)p.groups.size(), h->part_o, h->part_ml, h->o, h->o_dim, h->nq,
+                                   h->nkv, h->hd, h->bf16, s, h->kb_rows);
         });
       if (e != hipSuccess) break;
       GemmArgs go{};
