@@ -31,14 +31,28 @@
 namespace rosa {
 
 typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
+typedef __attribute__((ext_vector_type(32))) float f32x32;
 typedef __attribute__((ext_vector_type(6))) uint32_t u32x6;
+typedef __attribute__((ext_vector_type(6))) int i32x6;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+// A tile's rows in global memory: a uniform base (scalar registers) plus a per-lane byte offset.
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+__device__ __forceinline__ rsrc_t tile_rsrc(const uint8_t *base) {
+  const uint64_t b = (uint64_t)(size_t)base;
+  const uint64_t u = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  return __builtin_amdgcn_make_buffer_rsrc((void *)(size_t)u, 0, -1, 0x00027000);
+}
 
 // Every wave's LDS accesses so far are done before any wave goes on.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 // This wave's loads and copies have landed.
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(at::waitcnt_vm(0));
+  asm volatile("" ::: "memory");
+}
 
 template <int HD, int NG>
 struct Kv4Tile {
@@ -57,35 +71,50 @@ struct Kv4Tile {
   __device__ static int ksw(int row) { return (row >> SHIFT) & (CK - 1); }
 };
 
-// 32 consecutive query elements (16 words of bf16 pairs) as three 6-bit terms; returns
-// their scale bytes, first term's lowest.
+// Conversions of 32 elements on scale s to 6 bits and back.  In assembly for the early clobber:
+// they write their first result registers before they have read every source register, and the
+// builtins let the compiler put the result onto a source.
+__device__ __forceinline__ u32x6 to_fp6(const bf16x32 &v, float s) {
+  u32x6 t;
+  asm("v_cvt_scalef32_pk32_fp6_bf16 %0, %1, %2" : "=&v"(t) : "v"(v), "v"(s));
+  return t;
+}
+// element 2 i from a, 2 i + 1 from b
+__device__ __forceinline__ u32x6 to_fp6(const f32x16 &a, const f32x16 &b, float s) {
+  u32x6 t;
+  asm("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3" : "=&v"(t) : "v"(a), "v"(b), "v"(s));
+  return t;
+}
+__device__ __forceinline__ f32x32 from_fp6(const u32x6 &t, float s) {
+  f32x32 v;
+  asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2" : "=&v"(v) : "v"(t), "v"(s));
+  return v;
+}
+
+// 32 consecutive query elements as three 6-bit terms; returns the first one's scale byte (the
+// others' are 4 and 9 less), 255 where an element is not finite.
 __device__ __forceinline__ uint32_t split_query(const bf16x8 (&q)[4], u32x6 (&t)[3]) {
-  uint32_t w[16];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint4 u = __builtin_bit_cast(uint4, q[i]);
-    w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
-  }
+  f32x16 r[2];                               // even and odd elements
+  bf16x32 b;
   uint32_t a = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) a = max(a, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
+  for (int i = 0; i < 32; ++i) {
+    b[i] = q[i / 8][i % 8];
+    r[i & 1][i >> 1] = (float)b[i];
+    a = max(a, __float_as_uint((float)b[i]) & 0x7fffffffu);
+  }
   const int E = (int)(a >> 23) - 127;
   const int e = min(125, max(-115, (a & 0x7fffffu) <= 0x700000u ? E - 2 : E - 1));
-  bf16x32 r;
-  __builtin_memcpy(&r, w, sizeof r);
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const float s = __uint_as_float((uint32_t)(e + 127 - (k == 0 ? 0 : k == 1 ? 4 : 9)) << 23);
-    t[k] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(r, s);
+    t[k] = k == 0 ? to_fp6(b, s) : to_fp6(r[0], r[1], s);
     if (k == 2) break;
-    // what the term leaves: a multiple of the element's last bit and less than a step
-    // of the term, so exact in bf16
-    const bf16x32 b = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(t[k], s);
+    const f32x32 v = from_fp6(t[k], s);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) r[i] = (bf16)((float)r[i] - (float)b[i]);
+    for (int i = 0; i < 32; ++i) r[i & 1][i >> 1] -= v[i];     // exact: a multiple of the element's last bit
   }
-  // a NaN or an infinity in the block: every product with it is NaN
-  return a >= 0x7f800000u ? 0xffffffffu : (uint32_t)(e + 127) | (uint32_t)(e + 123) << 8 | (uint32_t)(e + 118) << 16;
+  return a >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
 }
 
 template <int HD, int NG>
@@ -116,36 +145,43 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
   const bool active = 32 * wave < it.nq;      // a wave without rows only helps with the copies
 
-  // Key range: prefix tiles [k0 + 32 t, + 32) with k0 = pe - 32 np (the first may
-  // reach below kbeg: masked), then own-key tiles likewise.
+  // Key range in tiles of 32 keys: np prefix tiles, then na of the request's own keys.  Tile 0 of
+  // each starts at the range's first key and gives its first pv0 (av0) keys; the others follow
+  // without a gap and end at the range's end, so tile 0's remaining rows are tile 1's
+  // first ones (masked here).  A range of fewer than 32 keys is one tile whose lanes past
+  // the end read its last row.  So every tile is a uniform base plus per-lane offsets fixed for the item.
   const int pe = min(it.kend, it.P), ab = max(it.kbeg, it.P);
-  const int np = pe > it.kbeg ? (pe - it.kbeg + 31) >> 5 : 0, k0 = pe - 32 * np;
-  const int na = it.kend > ab ? (it.kend - ab + 31) >> 5 : 0, a0 = it.kend - 32 * na;
+  const int pn = max(0, pe - it.kbeg), np = (pn + 31) >> 5, pv0 = pn - 32 * (np - 1);
+  const int an = max(0, it.kend - ab), na = (an + 31) >> 5, av0 = an - 32 * (na - 1);
+  auto atile = [&](int u) { return ab - it.P + (u == 0 ? 0 : 32 * (u - 1) + av0); };
 
-  const size_t rowb = (size_t)a.nkv * T::K4ROW, srow = (size_t)a.nkv * CK;
-  const size_t r0 = (size_t)a.layer * it.P * a.nkv + it.kvh, codes = kv4_code_bytes(ka.L, it.P, a.nkv, HD);
+  const uint32_t rowb = (uint32_t)a.nkv * T::K4ROW, srow = (uint32_t)a.nkv * CK;
+  const size_t r0 = ((size_t)a.layer * it.P + it.kbeg) * a.nkv + it.kvh, codes = kv4_code_bytes(ka.L, it.P, a.nkv, HD);
+  // the next tile to fetch: its codes and scales
   const uint8_t *kc = reinterpret_cast<const uint8_t *>(it.pk) + r0 * T::K4ROW;
   const uint8_t *vc = reinterpret_cast<const uint8_t *>(it.pv) + r0 * T::K4ROW;
   const uint8_t *ks = reinterpret_cast<const uint8_t *>(it.pk) + codes + r0 * CK;
   const uint8_t *vs = reinterpret_cast<const uint8_t *>(it.pv) + codes + r0 * CK;
 
   // ---- copies
-  // K codes of prefix tile t into ring stage t % 3: 1 KB a wave
-  auto copy_k4 = [&](int t) __attribute__((always_inline)) {
-    if (t >= np) return;
-    if (1024 * wave >= T::K4TILE || (T::K4TILE < 1024 && lane >= 32)) return;
-    const int p = wave * 64 + lane, row = p / CK, c = (p % CK) ^ T::ksw(row);
-    const int key = max(k0 + 32 * t + row, it.kbeg);
-    dma_1k(kc + (size_t)key * rowb + c * 16, lds0 + T::KOFF + (uint32_t)(t % 3) * T::K4TILE + wave * 1024);
-  };
+  // K codes of prefix tile t into ring stage t % 3: 1 KB a wave (head_dim 32: half of one)
+  constexpr bool K4HALF = T::K4TILE < 1024;
+  const bool k4on = 1024 * wave < T::K4TILE;
+  uint32_t koff;
+  {
+    const int p = wave * 64 + (K4HALF ? lane & 31 : lane), row = p / CK, c = (p % CK) ^ T::ksw(row);
+    koff = (uint32_t)min(row, pn - 1) * rowb + c * 16;
+  }
   // own keys: one bf16 tile (K or V columns) into LDS at dst
   auto copy_own = [&](int u, int col, uint32_t dst) __attribute__((always_inline)) {
     constexpr int UNITS = TILEB / 1024, RPU = 1024 / ROWB;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));             // recomputed at each use, not held through the key loop
 #pragma unroll
     for (int j = 0; j < (UNITS + 3) / 4; ++j) {
       if (4 * j + wave >= UNITS) continue;
-      const int row = (4 * j + wave) * RPU + lane / CPR, c = (lane % CPR) ^ at::swz(row, CPR);
-      const int key = max(a0 + 32 * u + row, ab) - it.P;
+      const int row = (4 * j + wave) * RPU + ln / CPR, c = (ln % CPR) ^ at::swz(row, CPR);
+      const int key = atile(u) + min(row, an - 1);
       dma_1k(qkv + (size_t)(it.tok_off + key) * a.ldqkv + col + c * 8, dst + (4 * j + wave) * 1024);
     }
   };
@@ -155,47 +191,67 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
 
   // V: this thread's block (vrow, vblk) of a tile, held from its load to its conversion one step
   // later.  Lanes are dealt so that the 16 of a group write distinct 16-byte columns.
-  int vrow, vblk;
-  if constexpr (HD == 256) {
-    vblk = (lane & 3) | ((lane >> 2) & 4);
-    vrow = (((lane >> 2) & 3) << 2) | (lane >> 5) | ((wave & 1) << 1) | ((wave >> 1) << 4);
-  } else if constexpr (HD == 128) {
-    vblk = lane & 3;
-    vrow = (((lane >> 2) & 3) << 2) | (lane >> 4) | ((wave & 1) << 4);
-  } else {
-    vblk = tid % CK;
-    vrow = (tid / CK) & 31;
-  }
-  uint4 vreg = make_uint4(0, 0, 0, 0);
-  uint32_t vscale = 0;
-  auto load_v = [&](int t) __attribute__((always_inline)) {
-    if (t >= np || tid >= HD) return;
-    const size_t key = (size_t)max(k0 + 32 * t + vrow, it.kbeg);
-    vreg = *reinterpret_cast<const uint4 *>(vc + key * rowb + vblk * 16);
-    vscale = vs[key * srow + vblk];
-  };
-  auto write_v = [&](int t) __attribute__((always_inline)) {
-    if (tid >= HD) return;
-    const float s = kv4_scale((uint8_t)vscale);
-    const uint32_t w[4] = {vreg.x, vreg.y, vreg.z, vreg.w};
-    uint8_t *dst = smem + (t & 1) * TILEB + vrow * ROWB;
-    const int sw = at::swz(vrow, CPR);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<bf16x8 *>(dst + (((4 * vblk + i) ^ sw) << 4)) = kv4_bf16x8(w[i], s);
-  };
-  // K scale bytes of this lane's row (lane & 31) of tile t, byte c for its block of product c
-  auto load_kscale = [&](int t) __attribute__((always_inline)) -> uint32_t {
-    const size_t key = (size_t)max(k0 + 32 * min(t, np - 1) + (lane & 31), it.kbeg);
-    const uint8_t *p = ks + key * srow;
-    if constexpr (CK == 8) {
-      const uint2 v = *reinterpret_cast<const uint2 *>(p);
-      return __builtin_amdgcn_perm(v.y, v.x, half ? 0x07050301u : 0x06040200u);
-    } else if constexpr (CK == 4) {
-      const uint32_t v = *reinterpret_cast<const uint32_t *>(p);
-      return __builtin_amdgcn_perm(0u, v, half ? 0x03030301u : 0x02020200u);
+  auto vblock = [&](int &vrow, int &vblk) __attribute__((always_inline)) {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));             // made at each use, not held through the key loop
+    if constexpr (HD == 256) {
+      vblk = (ln & 3) | ((ln >> 2) & 4);
+      vrow = (((ln >> 2) & 3) << 2) | (ln >> 5) | ((wave & 1) << 1) | ((wave >> 1) << 4);
+    } else if constexpr (HD == 128) {
+      vblk = ln & 3;
+      vrow = (((ln >> 2) & 3) << 2) | (ln >> 4) | ((wave & 1) << 4);
     } else {
-      return p[CK == 2 ? half : 0];
+      vblk = ln % CK;
+      vrow = (ln / CK) & 31;
     }
+  };
+  uint32_t voff;                             // a block's scale lies at 1/16 of its code offset
+  {
+    int vrow, vblk;
+    vblock(vrow, vblk);
+    voff = (uint32_t)min(vrow, pn - 1) * rowb + vblk * 16;
+  }
+  i32x4 vreg = {};
+  uint32_t vscale = 0;
+  const bool von = 64 * wave < HD;            // waves that convert (head_dim 32: half of one)
+  auto write_v = [&](int t) __attribute__((always_inline)) {
+    if (!von || (HD == 32 && half)) return;
+    const float s = kv4_scale((uint8_t)vscale);
+    int vrow, vblk;
+    vblock(vrow, vblk);
+    const uint32_t d = vstage(t) + (uint32_t)(vrow * ROWB + (((4 * vblk) ^ at::swz(vrow, CPR)) << 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<__attribute__((address_space(3))) bf16x8 *>((__attribute__((address_space(3))) uint8_t *)(size_t)(d ^ (i << 4))) =
+          kv4_bf16x8((uint32_t)vreg[i], s);
+  };
+  // K scale bytes of this lane's row (lane & 31)
+  u32x2 ksv = {};
+  // Prefix tile t on its way: K codes to ring stage t % 3, V and the scales to registers.  Tiles are
+  // fetched in order.
+  uint32_t kring = lds0 + T::KOFF + wave * 1024;
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    if (t >= np) return;
+    if (k4on && !(K4HALF && half)) dma_1k_s(kc, koff, kring);
+    if (von) {
+      vreg = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(tile_rsrc(vc), voff, 0, 0));
+      vscale = __builtin_amdgcn_raw_buffer_load_b8(tile_rsrc(vs), voff >> 4, 0, 0);
+    }
+    const rsrc_t p = tile_rsrc(ks);
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const uint32_t ksoff = (uint32_t)min(ln & 31, pn - 1) * srow;
+    if constexpr (CK == 8) ksv = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(p, ksoff, 0, 0));
+    else if constexpr (CK == 4) ksv[0] = __builtin_amdgcn_raw_buffer_load_b32(p, ksoff, 0, 0);
+    else ksv[0] = __builtin_amdgcn_raw_buffer_load_b8(p, ksoff + (CK == 2 ? half : 0), 0, 0);
+    kring = kring + T::K4TILE >= lds0 + T::KOFF + 3 * T::K4TILE ? kring - 2 * T::K4TILE : kring + T::K4TILE;
+    const uint32_t rows = t == 0 ? pv0 : 32;
+    kc += rows * rowb; vc += rows * rowb; ks += rows * srow; vs += rows * srow;
+  };
+  auto pick_kscale = [&](u32x2 v) __attribute__((always_inline)) -> uint32_t {
+    if constexpr (CK == 8) return __builtin_amdgcn_perm(v[1], v[0], half ? 0x07050301u : 0x06040200u);
+    else if constexpr (CK == 4) return __builtin_amdgcn_perm(0u, v[0], half ? 0x03030301u : 0x02020200u);
+    else return v[0];
   };
 
   // ---- LDS operand addresses
@@ -207,48 +263,49 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   // HD 32: 2 j + half
   const uint32_t abase = (uint32_t)(krow * ROWB + (((HD == 32 ? half : 4 * half) ^ at::swz(krow, CPR)) << 4));
   const int src16 = lane & 15, g16 = (lane >> 4) & 1;
-  uint32_t vbase[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = half * 4 + (src16 >> 2) + 8 * h;
-    const int sw = at::swz(r, CPR);
+  // source row 4 half + src16 / 4 (the pair's second 8 rows further: the swizzle's bit 1 turned)
+  uint32_t vbase;
+  {
+    const int r = half * 4 + (src16 >> 2), sw = at::swz(r, CPR);
     const int cl = (2 * g16 + ((src16 >> 1) & 1)) ^ (sw & 3);
-    vbase[h] = (uint32_t)(r * ROWB + 16 * cl + 8 * (src16 & 1)) ^ ((uint32_t)(sw >> 2) << 6);
+    vbase = (uint32_t)(r * ROWB + 16 * cl + 8 * (src16 & 1)) ^ ((uint32_t)(sw >> 2) << 6);
   }
 
   // ---- queries
-  const bf16 *qp[NG];
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const int loc = 32 * (wave + 4 * g) + (lane & 31);
+  auto query = [&](int g) __attribute__((always_inline)) -> const bf16 * {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int loc = 32 * (wave + 4 * g) + (ln & 31);
     const int qrow = it.q0 + (loc < it.nq ? loc : 0);   // rows past the item's: its first (never stored)
-    qp[g] = qkv + (size_t)(it.tok_off + qrow / G) * a.ldqkv + (size_t)(it.kvh * G + qrow % G) * HD;
-  }
+    return qkv + (size_t)(it.tok_off + qrow / G) * a.ldqkv + (size_t)(it.kvh * G + qrow % G) * HD;
+  };
 
   f32x16 o[NG][NT];
   float m_ref[NG], l_run[NG];
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    m_ref[g] = -INFINITY;
-    l_run[g] = 0.f;
+    for (int g = 0; g < NG; ++g) {
+      m_ref[g] = -INFINITY;
+      l_run[g] = 0.f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[g][n][r] = 0.f;
-  }
+        for (int r = 0; r < 16; ++r) o[g][n][r] = 0.f;
+    }
+  };
 
   // Softmax of one tile of scores (register r: key (r/4)*8 + 4 half + r%4) into P^T.
   // Weights are 2^((s - m_ref) sl2) against a reference that is the first tile's maximum and
   // moves (with O and the sum rescaled) only when a score exceeds it by 2^32 in weight: weights
   // and sums stay far from overflow, and the accumulators are left alone nearly always.
-  // lo: keys of the tile below this index are masked.
-  auto softmax = [&](f32x16 (&s)[NG], bf16x8 (&pp)[NG][2], int lo) __attribute__((always_inline)) {
+  // Keys of the tile from index n_keys on are masked.
+  auto softmax = [&](f32x16 (&s)[NG], bf16x8 (&pp)[NG][2], int n_keys) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      if (lo > 0) {
+      if (n_keys < 32) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if ((r >> 2) * 8 + half * 4 + (r & 3) < lo) s[g][r] = -INFINITY;
+          if ((r >> 2) * 8 + half * 4 + (r & 3) >= n_keys) s[g][r] = -INFINITY;
       }
       float tmax = fmaxf(s[g][0], s[g][1]);
 #pragma unroll
@@ -287,11 +344,12 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   };
   // O^T += V^T P^T over the V tile at vst
   auto pv_acc = [&](uint32_t vst, const bf16x8 (&pp)[NG][2]) __attribute__((always_inline)) {
-    const uint32_t v0 = vst + vbase[0], v1 = vst + vbase[1];
+    const uint32_t v0 = vst + vbase;
     auto vfrag = [&](int j) __attribute__((always_inline)) -> bf16x8 {
       const int kk = j / NT, n = j % NT, c = (n / 4) * 256 + kk * 16 * ROWB;
       const uint32_t x = (uint32_t)(64 * (n % 4));
-      return lds_tr_pair(lds_ptr(v0 ^ x) + c, lds_ptr(v1 ^ x) + c);
+      constexpr uint32_t x8 = CPR >= 4 ? 32 : 0;
+      return lds_tr_pair(lds_ptr(v0 ^ x) + c, lds_ptr(v0 ^ x ^ x8) + c + 8 * ROWB);
     };
     constexpr int NJ = 2 * NT;
     bf16x8 fr[3];
@@ -309,97 +367,118 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
 
   // ---- prologue: the first tiles' copies, then the queries
   if (np > 0) {
-    copy_k4(0);
-    copy_k4(1);
-    load_v(0);
+    fetch(0);
   } else {
     copy_own(0, kcol, astage(0));
     copy_own(0, vcol, vstage(0));
   }
-  if (np > 0) {
+  if (np == 0) {
+    clear();
+  } else {
     u32x6 q6[NG][NCH][3];
-    uint32_t qs[NG][NCH];
+    uint32_t qs[NG][3] = {};                // byte c: the scale of product c's block, per term
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
+    for (int g = 0; g < NG; ++g) {
+      const bf16 *qp = query(g);
 #pragma unroll
       for (int c = 0; c < NCH; ++c) {
         bf16x8 q[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          q[j] = *reinterpret_cast<const bf16x8 *>(qp[g] + 64 * c + (HD == 32 ? 0 : 32 * half) + 8 * j);
+          q[j] = *reinterpret_cast<const bf16x8 *>(qp + 64 * c + (HD == 32 ? 0 : 32 * half) + 8 * j);
           if (HD == 32 && half) q[j] = bf16x8{};        // a product is 64 wide
         }
-        qs[g][c] = split_query(q, q6[g][c]);
+        const uint32_t e0 = split_query(q, q6[g][c]);
+        // a NaN or an infinity in the block: every product with it is NaN
+#pragma unroll
+        for (int k = 0; k < 3; ++k) qs[g][k] |= (e0 == 255 ? 255u : e0 - (k == 0 ? 0 : k == 1 ? 4 : 9)) << (8 * c);
       }
+    }
+    clear();
     wait_loads();
     write_v(0);
-    load_v(1);
-    uint32_t ksc = load_kscale(0);
+    uint32_t ksc = pick_kscale(ksv);
+    fetch(1);
+    uint32_t kst = k4base;                  // the lane's row in the tile's ring stage
+    auto key_loop = [&](auto act) __attribute__((always_inline)) {
     for (int t = 0; t < np; ++t) {
       lds_barrier();                        // tile t is in LDS; every wave is done with tile t - 1
-      const uint32_t ksn = load_kscale(t + 1);
       f32x16 s[NG];
       bf16x8 pp[NG][2];
-      if (active) {
-        const uint32_t kb = k4base + (uint32_t)(t % 3) * T::K4TILE;
+      if constexpr (act.value) {
+        auto kfrag = [&](int c) __attribute__((always_inline)) -> i32x4 {
+          const i32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(lds_ptr(kst ^ (uint32_t)(32 * c)));
+          return HD == 32 && half ? i32x4{} : k;
+        };
+        i32x4 kr[2];                        // codes are read one product ahead
+        kr[0] = kfrag(0);
+        if (NCH > 1) kr[1] = kfrag(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-          i32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(lds_ptr(kb ^ (uint32_t)(32 * c)));
-          if (HD == 32 && half) k = i32x4{};
-          const i32x8 kf = {k[0], k[1], k[2], k[3], 0, 0, 0, 0};
+          const i32x4 k = kr[c & 1];
+          const i32x8 kf = __builtin_shufflevector(k, k, 0, 1, 2, 3, -1, -1, -1, -1);   // a 4-bit operand is 4 registers
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             auto term = [&](auto kk) __attribute__((always_inline)) {
               constexpr int K = decltype(kk)::value;
-              const u32x6 &x = q6[g][c][K];
-              const i32x8 qf = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+              const i32x6 x = __builtin_bit_cast(i32x6, q6[g][c][K]);
+              const i32x8 qf = __builtin_shufflevector(x, x, 0, 1, 2, 3, 4, 5, -1, -1);
               const f32x16 acc = c == 0 && K == 0 ? f32x16{} : s[g];
-              if (c == 0) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 0, ksc, K, qs[g][c]);
-              if (c == 1) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 1, ksc, K, qs[g][c]);
-              if (c == 2) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 2, ksc, K, qs[g][c]);
-              if (c == 3) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 3, ksc, K, qs[g][c]);
+              if (c == 0) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 0, ksc, 0, qs[g][K]);
+              if (c == 1) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 1, ksc, 1, qs[g][K]);
+              if (c == 2) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 2, ksc, 2, qs[g][K]);
+              if (c == 3) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 3, ksc, 3, qs[g][K]);
             };
             term(std::integral_constant<int, 0>{});
             term(std::integral_constant<int, 1>{});
             term(std::integral_constant<int, 2>{});
           }
+          if (c + 2 < NCH) kr[c & 1] = kfrag(c + 2);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        softmax(s, pp, t == 0 ? it.kbeg - k0 : 0);
+        softmax(s, pp, t == 0 ? pv0 : 32);
       }
       // V of tile t + 1 to the other stage; then the loads for the tiles behind it.
       // K codes t + 1 landed with V (issued before it).
       wait_loads();
       if (t + 1 < np) {
+        ksc = pick_kscale(ksv);
         write_v(t + 1);
-        copy_k4(t + 2);
-        load_v(t + 2);
+        fetch(t + 2);
+        kst = (t + 1) % 3 == 0 ? kst - 2 * T::K4TILE : kst + T::K4TILE;
       } else if (na > 0) {
         copy_own(0, kcol, astage(t + 1));
         copy_own(0, vcol, vstage(t + 1));
       }
-      ksc = ksn;
       __builtin_amdgcn_sched_barrier(0);
-      if (active) pv_acc(vstage(t), pp);
+      if constexpr (act.value) pv_acc(vstage(t), pp);
     }
+    };
+    if (active) key_loop(std::true_type{});
+    else key_loop(std::false_type{});
   }
   // ---- the request's own keys
   if (na > 0) {
     bf16x8 qf[NG][NS];
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
+    for (int g = 0; g < NG; ++g) {
+      const bf16 *qp = query(g);
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         // fragment i: elements 64 (i / 4) + 32 half + 8 (i % 4) (HD 32: 16 i + 8 half)
         const int at = HD == 32 ? 16 * i + 8 * half : 64 * (i / 4) + 32 * half + 8 * (i % 4);
-        qf[g][i] = *reinterpret_cast<const bf16x8 *>(qp[g] + at);
+        qf[g][i] = *reinterpret_cast<const bf16x8 *>(qp + at);
       }
+    }
+    auto own_loop = [&](auto act) __attribute__((always_inline)) {
     for (int u = 0; u < na; ++u) {
       const int t = np + u;
       wait_loads();
       lds_barrier();
       f32x16 s[NG];
       bf16x8 pp[NG][2];
-      if (active) {
+      if constexpr (act.value) {
         const uint32_t ab0 = astage(t) + abase;
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
@@ -409,15 +488,18 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
           for (int g = 0; g < NG; ++g)
             s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[g][i], i == 0 ? f32x16{} : s[g], 0, 0, 0);
         }
-        softmax(s, pp, u == 0 ? ab - a0 : 0);
+        softmax(s, pp, u == 0 ? av0 : 32);
       }
       if (u + 1 < na) {
         copy_own(u + 1, kcol, astage(t + 1));
         copy_own(u + 1, vcol, vstage(t + 1));
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (active) pv_acc(vstage(t), pp);
+      if constexpr (act.value) pv_acc(vstage(t), pp);
     }
+    };
+    if (active) own_loop(std::true_type{});
+    else own_loop(std::false_type{});
   }
   wait_loads();
   lds_barrier();                          // every wave is done with the rings
