@@ -228,10 +228,10 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   // K scale bytes of this lane's row (lane & 31)
   u32x2 ksv = {};
   // Prefix tile t on its way: K codes to ring stage t % 3, V and the scales to registers.  Tiles are
-  // fetched in order.
+  // fetched in order; past the last one it is fetched again, into what nothing reads, so that no
+  // branch (whose joined registers would have to be waited for) stands in the key loop.
   uint32_t kring = lds0 + T::KOFF + wave * 1024;
   auto fetch = [&](int t) __attribute__((always_inline)) {
-    if (t >= np) return;
     if (k4on && !(K4HALF && half)) dma_1k_s(kc, koff, kring);
     if (von) {
       vreg = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(tile_rsrc(vc), voff, 0, 0));
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
     else if constexpr (CK == 4) ksv[0] = __builtin_amdgcn_raw_buffer_load_b32(p, ksoff, 0, 0);
     else ksv[0] = __builtin_amdgcn_raw_buffer_load_b8(p, ksoff + (CK == 2 ? half : 0), 0, 0);
     kring = kring + T::K4TILE >= lds0 + T::KOFF + 3 * T::K4TILE ? kring - 2 * T::K4TILE : kring + T::K4TILE;
-    const uint32_t rows = t == 0 ? pv0 : 32;
+    const uint32_t rows = t + 1 >= np ? 0 : t == 0 ? pv0 : 32;
     kc += rows * rowb; vc += rows * rowb; ks += rows * srow; vs += rows * srow;
   };
   auto pick_kscale = [&](u32x2 v) __attribute__((always_inline)) -> uint32_t {
@@ -281,11 +281,12 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   };
 
   f32x16 o[NG][NT];
-  float m_ref[NG], l_run[NG];
+  // negative reference of the row's weights in log2 units (3e38: none yet), their sum
+  float mb[NG], l_run[NG];
   auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      m_ref[g] = -INFINITY;
+      mb[g] = 3e38f;
       l_run[g] = 0.f;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   };
 
   // Softmax of one tile of scores (register r: key (r/4)*8 + 4 half + r%4) into P^T.
-  // Weights are 2^((s - m_ref) sl2) against a reference that is the first tile's maximum and
+  // Weights are 2^(s sl2 + mb) against a reference that is the first tile's maximum and
   // moves (with O and the sum rescaled) only when a score exceeds it by 2^32 in weight: weights
   // and sums stay far from overflow, and the accumulators are left alone nearly always.
   // Keys of the tile from index n_keys on are masked.
@@ -310,20 +311,20 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
       float tmax = fmaxf(s[g][0], s[g][1]);
 #pragma unroll
       for (int r = 2; r < 16; ++r) tmax = fmaxf(tmax, s[g][r]);
-      if (__ballot((tmax - m_ref[g]) * sl2 > 32.0f)) {    // also every first tile (m_ref = -inf)
+      if (__ballot(fmaf(tmax, sl2, mb[g]) > 32.0f)) {     // also every first tile
         const float tm = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-        const bool up = (tm - m_ref[g]) * sl2 > 32.0f;    // the halves of a query agree
-        const float f = up ? __builtin_amdgcn_exp2f((m_ref[g] - tm) * sl2) : 1.0f;
-        if (up) m_ref[g] = tm;
+        const bool up = fmaf(tm, sl2, mb[g]) > 32.0f;     // the halves of a query agree
+        const float nb = up ? -tm * sl2 : mb[g];
+        const float f = up ? __builtin_amdgcn_exp2f(nb - mb[g]) : 1.0f;
+        mb[g] = nb;
         l_run[g] *= f;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[g][n][r] *= f;
       }
-      const float mb = m_ref[g] == -INFINITY ? 0.f : -m_ref[g] * sl2;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[g][r] = __builtin_amdgcn_exp2f(fmaf(s[g][r], sl2, mb));
+      for (int r = 0; r < 16; ++r) s[g][r] = __builtin_amdgcn_exp2f(fmaf(s[g][r], sl2, mb[g]));
       float ps = 0.f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -442,15 +443,15 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
       // V of tile t + 1 to the other stage; then the loads for the tiles behind it.
       // K codes t + 1 landed with V (issued before it).
       wait_loads();
+      ksc = pick_kscale(ksv);
+      kst = (t + 1) % 3 == 0 ? kst - 2 * T::K4TILE : kst + T::K4TILE;
       if (t + 1 < np) {
-        ksc = pick_kscale(ksv);
         write_v(t + 1);
-        fetch(t + 2);
-        kst = (t + 1) % 3 == 0 ? kst - 2 * T::K4TILE : kst + T::K4TILE;
       } else if (na > 0) {
         copy_own(0, kcol, astage(t + 1));
         copy_own(0, vcol, vstage(t + 1));
       }
+      fetch(t + 2);
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (act.value) pv_acc(vstage(t), pp);
     }
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
     const float l = l_run[g] + __shfl_xor(l_run[g], 32, 64);
     const int loc = 32 * (wave + 4 * g) + (lane & 31);
     if (loc >= it.nq) continue;
-    const float m2 = m_ref[g] * sl2;                      // log2 units
+    const float m2 = -mb[g];                              // log2 units
     if (it.slot >= 0) {
       const size_t pr = (size_t)it.slot * kAttnQB + loc;
       float *po = reinterpret_cast<float *>(a.part_o) + pr * HD + 4 * half;
