@@ -76,23 +76,24 @@ struct Kv4Tile {
 // builtins let the compiler put the result onto a source.
 __device__ __forceinline__ u32x6 to_fp6(const bf16x32 &v, float s) {
   u32x6 t;
-  asm("v_cvt_scalef32_pk32_fp6_bf16 %0, %1, %2" : "=&v"(t) : "v"(v), "v"(s));
+  asm volatile("v_cvt_scalef32_pk32_fp6_bf16 %0, %1, %2" : "=&v"(t) : "v"(v), "v"(s));
   return t;
 }
 // element 2 i from a, 2 i + 1 from b
 __device__ __forceinline__ u32x6 to_fp6(const f32x16 &a, const f32x16 &b, float s) {
   u32x6 t;
-  asm("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3" : "=&v"(t) : "v"(a), "v"(b), "v"(s));
+  asm volatile("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3" : "=&v"(t) : "v"(a), "v"(b), "v"(s));
   return t;
 }
 __device__ __forceinline__ f32x32 from_fp6(const u32x6 &t, float s) {
   f32x32 v;
-  asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2" : "=&v"(v) : "v"(t), "v"(s));
+  asm volatile("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2" : "=&v"(v) : "v"(t), "v"(s));
   return v;
 }
 
 // 32 consecutive query elements as three 6-bit terms; returns the first one's scale byte (the
-// others' are 4 and 9 less), 255 where an element is not finite.
+// others' are 4 and 9 less), 255 where an element is not finite (every product with the first
+// term is then NaN).
 __device__ __forceinline__ uint32_t split_query(const bf16x8 (&q)[4], u32x6 (&t)[3]) {
   f32x16 r[2];                               // even and odd elements
   bf16x32 b;
@@ -214,19 +215,19 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   i32x4 vreg = {};
   uint32_t vscale = 0;
   const bool von = 64 * wave < HD;            // waves that convert (head_dim 32: half of one)
-  auto write_v = [&](int t) __attribute__((always_inline)) {
-    if (!von || (HD == 32 && half)) return;
-    const float s = kv4_scale((uint8_t)vscale);
+  // bf16 of the block's words 0 .. 3, one at a time, into the V tile at dst
+  auto v_dst = [&](uint32_t dst) __attribute__((always_inline)) -> uint32_t {
     int vrow, vblk;
     vblock(vrow, vblk);
-    const uint32_t d = vstage(t) + (uint32_t)(vrow * ROWB + (((4 * vblk) ^ at::swz(vrow, CPR)) << 4));
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<__attribute__((address_space(3))) bf16x8 *>((__attribute__((address_space(3))) uint8_t *)(size_t)(d ^ (i << 4))) =
-          kv4_bf16x8((uint32_t)vreg[i], s);
+    return dst + (uint32_t)(vrow * ROWB + (((4 * vblk) ^ at::swz(vrow, CPR)) << 4));
   };
-  // K scale bytes of this lane's row (lane & 31)
-  u32x2 ksv = {};
+  auto write_v = [&](uint32_t d, int i) __attribute__((always_inline)) {
+    if (!von || (HD == 32 && half)) return;
+    *reinterpret_cast<__attribute__((address_space(3))) bf16x8 *>((__attribute__((address_space(3))) uint8_t *)(size_t)(d ^ (i << 4))) =
+        kv4_bf16x8((uint32_t)vreg[i], kv4_scale((uint8_t)vscale));
+  };
+  // K scale bytes of this lane's row (lane & 31): of its half's blocks, NCH half + c in byte c
+  uint32_t ksv = 0;
   // Prefix tile t on its way: K codes to ring stage t % 3, V and the scales to registers.  Tiles are
   // fetched in order; past the last one it is fetched again, into what nothing reads, so that no
   // branch (whose joined registers would have to be waited for) stands in the key loop.
@@ -235,30 +236,26 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
     if (k4on && !(K4HALF && half)) dma_1k_s(kc, koff, kring);
     if (von) {
       vreg = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(tile_rsrc(vc), voff, 0, 0));
-      vscale = __builtin_amdgcn_raw_buffer_load_b8(tile_rsrc(vs), voff >> 4, 0, 0);
+      uint32_t vo = voff;
+      asm volatile("" : "+v"(vo));
+      vscale = __builtin_amdgcn_raw_buffer_load_b8(tile_rsrc(vs), vo >> 4, 0, 0);
     }
     const rsrc_t p = tile_rsrc(ks);
     int ln = lane;
     asm volatile("" : "+v"(ln));
-    const uint32_t ksoff = (uint32_t)min(ln & 31, pn - 1) * srow;
-    if constexpr (CK == 8) ksv = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(p, ksoff, 0, 0));
-    else if constexpr (CK == 4) ksv[0] = __builtin_amdgcn_raw_buffer_load_b32(p, ksoff, 0, 0);
-    else ksv[0] = __builtin_amdgcn_raw_buffer_load_b8(p, ksoff + (CK == 2 ? half : 0), 0, 0);
+    const uint32_t ksoff = (uint32_t)min(ln & 31, pn - 1) * srow + (CK > 1 ? (uint32_t)(ln >> 5) * NCH : 0u);
+    if constexpr (CK == 8) ksv = __builtin_amdgcn_raw_buffer_load_b32(p, ksoff, 0, 0);
+    else if constexpr (CK == 4) ksv = __builtin_amdgcn_raw_buffer_load_b16(p, ksoff, 0, 0);
+    else ksv = __builtin_amdgcn_raw_buffer_load_b8(p, ksoff, 0, 0);
     kring = kring + T::K4TILE >= lds0 + T::KOFF + 3 * T::K4TILE ? kring - 2 * T::K4TILE : kring + T::K4TILE;
     const uint32_t rows = t + 1 >= np ? 0 : t == 0 ? pv0 : 32;
     kc += rows * rowb; vc += rows * rowb; ks += rows * srow; vs += rows * srow;
   };
-  auto pick_kscale = [&](u32x2 v) __attribute__((always_inline)) -> uint32_t {
-    if constexpr (CK == 8) return __builtin_amdgcn_perm(v[1], v[0], half ? 0x07050301u : 0x06040200u);
-    else if constexpr (CK == 4) return __builtin_amdgcn_perm(0u, v[0], half ? 0x03030301u : 0x02020200u);
-    else return v[0];
-  };
-
   // ---- LDS operand addresses
   const int krow = lane & 31;
-  // code chunk 2 c + half of the lane's row: base ^ 32 c (rows and stages are multiples of the
+  // code chunk NCH half + c of the lane's row: base ^ 16 c (rows and stages are multiples of the
   // swizzled bits' span)
-  const uint32_t k4base = lds0 + T::KOFF + krow * T::K4ROW + (CK == 1 ? 0 : ((half ^ T::ksw(krow)) << 4));
+  const uint32_t k4base = lds0 + T::KOFF + krow * T::K4ROW + (CK == 1 ? 0 : (((NCH * half) ^ T::ksw(krow)) << 4));
   // own-key K chunk HD >= 64: 8 c + 4 half + j (a lane's elements 32 consecutive, as in the codes),
   // HD 32: 2 j + half
   const uint32_t abase = (uint32_t)(krow * ROWB + (((HD == 32 ? half : 4 * half) ^ at::swz(krow, CPR)) << 4));
@@ -283,7 +280,10 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   f32x16 o[NG][NT];
   // negative reference of the row's weights in log2 units (3e38: none yet), their sum
   float mb[NG], l_run[NG];
+  // (behind the queries' conversion, volatile too: both at once need more registers than there are)
   auto clear = [&]() __attribute__((always_inline)) {
+    float z;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(z));
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       mb[g] = 3e38f;
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[g][n][r] = 0.f;
+        for (int r = 0; r < 16; ++r) o[g][n][r] = z;
     }
   };
 
@@ -348,9 +348,10 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
     const uint32_t v0 = vst + vbase;
     auto vfrag = [&](int j) __attribute__((always_inline)) -> bf16x8 {
       const int kk = j / NT, n = j % NT, c = (n / 4) * 256 + kk * 16 * ROWB;
-      const uint32_t x = (uint32_t)(64 * (n % 4));
-      constexpr uint32_t x8 = CPR >= 4 ? 32 : 0;
-      return lds_tr_pair(lds_ptr(v0 ^ x) + c, lds_ptr(v0 ^ x ^ x8) + c + 8 * ROWB);
+      uint32_t v = v0;
+      if (HD == 256) asm volatile("" : "+v"(v));   // addresses made at each use: registers are short
+      v ^= (uint32_t)(64 * (n % 4));
+      return lds_tr_pair(lds_ptr(v) + c, lds_ptr(v ^ 32u) + c + 8 * ROWB);
     };
     constexpr int NJ = 2 * NT;
     bf16x8 fr[3];
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
     clear();
   } else {
     u32x6 q6[NG][NCH][3];
-    uint32_t qs[NG][3] = {};                // byte c: the scale of product c's block, per term
+    uint32_t qs[NG] = {};                   // byte c: the scale of product c's block, first term
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       const bf16 *qp = query(g);
@@ -386,29 +387,45 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
         bf16x8 q[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          q[j] = *reinterpret_cast<const bf16x8 *>(qp + 64 * c + (HD == 32 ? 0 : 32 * half) + 8 * j);
+          q[j] = *reinterpret_cast<const bf16x8 *>(qp + 32 * c + (HD == 32 ? 0 : 32 * NCH * half) + 8 * j);
           if (HD == 32 && half) q[j] = bf16x8{};        // a product is 64 wide
         }
-        const uint32_t e0 = split_query(q, q6[g][c]);
-        // a NaN or an infinity in the block: every product with it is NaN
-#pragma unroll
-        for (int k = 0; k < 3; ++k) qs[g][k] |= (e0 == 255 ? 255u : e0 - (k == 0 ? 0 : k == 1 ? 4 : 9)) << (8 * c);
+        qs[g] |= split_query(q, q6[g][c]) << (8 * c);
       }
     }
     clear();
     wait_loads();
-    write_v(0);
-    uint32_t ksc = pick_kscale(ksv);
+    {
+      const uint32_t d = v_dst(vstage(0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) write_v(d, i);
+    }
+    uint32_t ksc = ksv;
     fetch(1);
     uint32_t kst = k4base;                  // the lane's row in the tile's ring stage
     auto key_loop = [&](auto act) __attribute__((always_inline)) {
     for (int t = 0; t < np; ++t) {
       lds_barrier();                        // tile t is in LDS; every wave is done with tile t - 1
+      wait_loads();                         // K codes, V and scales of tile t + 1
+      // Runs in the shadow of the last score products, where registers are free: V of tile t + 1 to
+      // the other stage (behind the last tile to the own-key stage that is still free), then the
+      // next copies.
+      uint32_t d = 0, ksn = 0;
+      auto next = [&](int c) __attribute__((always_inline)) {
+        constexpr int C0 = NCH > 1 ? NCH - 2 : 0;
+        if (c == C0) d = v_dst(t + 1 < np ? vstage(t + 1) : astage(t));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c == C0 + (NCH > 1 ? i / 2 : 0)) write_v(d, i);
+        if (c < NCH - 1) return;
+        ksn = ksv;
+        fetch(t + 2);
+      };
       f32x16 s[NG];
       bf16x8 pp[NG][2];
       if constexpr (act.value) {
         auto kfrag = [&](int c) __attribute__((always_inline)) -> i32x4 {
-          const i32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(lds_ptr(kst ^ (uint32_t)(32 * c)));
+          const i32x4 k = *reinterpret_cast<const __attribute__((address_space(3))) i32x4 *>(lds_ptr(kst ^ (uint32_t)(16 * c)));
           return HD == 32 && half ? i32x4{} : k;
         };
         i32x4 kr[2];                        // codes are read one product ahead
@@ -425,35 +442,37 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
               constexpr int K = decltype(kk)::value;
               const i32x6 x = __builtin_bit_cast(i32x6, q6[g][c][K]);
               const i32x8 qf = __builtin_shufflevector(x, x, 0, 1, 2, 3, 4, 5, -1, -1);
+              uint32_t sc = qs[g];          // the terms' scales are 4 and 9 below the first's
+              if (K > 0) asm volatile("" : "+v"(sc));
+              sc -= K == 0 ? 0u : K == 1 ? 0x04040404u : 0x09090909u;
               const f32x16 acc = c == 0 && K == 0 ? f32x16{} : s[g];
-              if (c == 0) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 0, ksc, 0, qs[g][K]);
-              if (c == 1) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 1, ksc, 1, qs[g][K]);
-              if (c == 2) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 2, ksc, 2, qs[g][K]);
-              if (c == 3) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 3, ksc, 3, qs[g][K]);
+              if (c == 0) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 0, ksc, 0, sc);
+              if (c == 1) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 1, ksc, 1, sc);
+              if (c == 2) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 2, ksc, 2, sc);
+              if (c == 3) s[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, qf, acc, 4, 2, 3, ksc, 3, sc);
             };
             term(std::integral_constant<int, 0>{});
             term(std::integral_constant<int, 1>{});
             term(std::integral_constant<int, 2>{});
           }
           if (c + 2 < NCH) kr[c & 1] = kfrag(c + 2);
+          next(c);
           __builtin_amdgcn_sched_barrier(0);
         }
         softmax(s, pp, t == 0 ? pv0 : 32);
       }
-      // V of tile t + 1 to the other stage; then the loads for the tiles behind it.
-      // K codes t + 1 landed with V (issued before it).
-      wait_loads();
-      ksc = pick_kscale(ksv);
-      kst = (t + 1) % 3 == 0 ? kst - 2 * T::K4TILE : kst + T::K4TILE;
-      if (t + 1 < np) {
-        write_v(t + 1);
-      } else if (na > 0) {
+      else {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) next(c);
+      }
+      if (t + 1 == np && na > 0) {
         copy_own(0, kcol, astage(t + 1));
         copy_own(0, vcol, vstage(t + 1));
       }
-      fetch(t + 2);
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (act.value) pv_acc(vstage(t), pp);
+      ksc = ksn;
+      kst = (t + 1) % 3 == 0 ? kst - 2 * T::K4TILE : kst + T::K4TILE;
     }
     };
     if (active) key_loop(std::true_type{});
