@@ -26,7 +26,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librosa.so")
 LIB_SAN = os.path.join(PKG, "librosa_san.so")
-SOURCES = ["k_time.hip", "k_rows.hip", "k_gemm.hip", "k_attn.hip", "k_probe.hip", "k_prefill.hip", "k_kv.hip", "k_kvattn.hip",
+SOURCES = ["k_time.hip", "k_rows.hip", "k_gemm.hip", "k_attn.hip", "k_probe.hip", "k_prefill.hip", "k_kv.hip", "k_kvattn.hip", "k_kvmass.hip",
            "rosa_api.cpp", "rosa_prefill.cpp", "rosa_sched.cpp", "rosa_kv.cpp"]
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall", "-Wno-unused-result",

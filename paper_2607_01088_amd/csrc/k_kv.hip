@@ -389,22 +389,22 @@ hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16_mode, hipStre
 }
 
 // ------------------------------------------------------------------ attention weight of cached tokens
-// mass_j = sum over the KV head's query rows r of exp(q_r . k_j / sqrt(hd) - lse_r).  A
-// block holds kMassKeys keys, a wave one of them at a time; its lane groups take
+// mass_j = sum over the KV head's query rows r of exp(q_r . k_j / sqrt(hd) - lse_r).  fp32 mode: a
+// block holds kMassRows keys, a wave one of them at a time; its lane groups take
 // every NG-th query row.
-template <int HD, typename T, bool FP4>
+template <int HD, bool FP4>
 __global__ void __launch_bounds__(256) kv_mass_rows_kernel(KvMassArgs a) {
   constexpr int LG = HD / 16, NG = 64 / LG;
   const MassItem it = a.items[blockIdx.x];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % LG, g = lane / LG;
   const int G = a.nq / a.nkv, R = it.H * G;
-  const T *qkv = reinterpret_cast<const T *>(a.qkv);
+  const float *qkv = reinterpret_cast<const float *>(a.qkv);
   const size_t codes = kv4_code_bytes(a.L, it.P, a.nkv, HD);
   const float scale = 1.0f / sqrtf((float)HD);
   for (int kk = wave; kk < it.nk; kk += 4) {
     const int key = it.k0 + kk;
     float kf[16];
-    load16_cache<HD, T, FP4>(it.pk, codes, ((size_t)a.layer * it.P + key) * a.nkv + it.kvh, c, kf);
+    load16_cache<HD, float, FP4>(it.pk, codes, ((size_t)a.layer * it.P + key) * a.nkv + it.kvh, c, kf);
     float sum = 0.f;
     for (int r0 = 0; r0 < R; r0 += NG) {
       const int r = min(r0 + g, R - 1);
@@ -428,24 +428,17 @@ __global__ void __launch_bounds__(256) kv_mass_rows_kernel(KvMassArgs a) {
 }
 
 template <int HD>
-static void launch_mass_rows(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
-  dim3 grid(a.n_items);
-  if (bf16_mode) {
-    if (a.fp4) hipLaunchKernelGGL((kv_mass_rows_kernel<HD, bf16, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((kv_mass_rows_kernel<HD, bf16, false>), grid, dim3(256), 0, s, a);
-  } else {
-    if (a.fp4) hipLaunchKernelGGL((kv_mass_rows_kernel<HD, float, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((kv_mass_rows_kernel<HD, float, false>), grid, dim3(256), 0, s, a);
-  }
+static void launch_mass_rows(const KvMassArgs &a, hipStream_t s) {
+  if (a.fp4) hipLaunchKernelGGL((kv_mass_rows_kernel<HD, true>), dim3(a.n_items), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_mass_rows_kernel<HD, false>), dim3(a.n_items), dim3(256), 0, s, a);
 }
 
-hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
-  if (a.n_items <= 0) return hipSuccess;
+hipError_t launch_kv_mass_rows(const KvMassArgs &a, hipStream_t s) {
   switch (a.hd) {
-    case 32: launch_mass_rows<32>(a, bf16_mode, s); break;
-    case 64: launch_mass_rows<64>(a, bf16_mode, s); break;
-    case 128: launch_mass_rows<128>(a, bf16_mode, s); break;
-    case 256: launch_mass_rows<256>(a, bf16_mode, s); break;
+    case 32: launch_mass_rows<32>(a, s); break;
+    case 64: launch_mass_rows<64>(a, s); break;
+    case 128: launch_mass_rows<128>(a, s); break;
+    case 256: launch_mass_rows<256>(a, s); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

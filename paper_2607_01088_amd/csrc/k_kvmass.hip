@@ -1,0 +1,215 @@
+// Attention weight of cached tokens on the matrix cores (gfx950), bf16 mode, one layer:
+//   mass_j = sum over the KV head's query rows r of exp(q_r . k_j / sqrt(hd) - lse_r).
+//
+// S = Q K^T in 32 x 32 tiles with a key to each lane: the sum over query rows is then a sum over a lane's
+// registers.  The keys stay, the queries pass: a wave holds KT tiles of 32 keys in registers (a 4-bit
+// cache's turned to bf16 there, exactly, once for all queries, so both formats share the products), and the
+// block's queries come by through a ring in LDS.  A block's waves take WK different groups of keys and 4 / WK
+// different tiles of queries; each key's sum is made by one block in a fixed order (no atomics).
+// 256 requests of 512 to 1280 cached tokens, 16 or 50 action tokens x 8 heads, head_dim 256: 66 us over
+// a bf16 cache (a key at a time on the vector units: 2220), 57 us over a 4-bit one; one request's 816
+// tokens under 50: 11 (385).  Bounds: the products take 14 us of the matrix cores, K 24 us (bf16) of HBM.
+#include <math.h>
+
+#include "rosa_device.h"
+#include "rosa_internal.h"
+
+namespace rosa {
+
+// 64 floats, each lane's from its own address, to lds + 4 lane
+__device__ __forceinline__ void dma_256(const float *src, uint32_t lds) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
+// A lane's half of a cached row (HD / 2 elements) in bf16, in the order of its operands: bf16 cache, operand i: 8
+// elements from 16 i + 8 half on; 4-bit cache: 8 from HD / 2 half + 8 i on (whole blocks, or half of one).
+template <int HD>
+__device__ __forceinline__ void read_key(const KvMassArgs &a, const MassItem &it, int key, int half, bool fp4, bf16x8 (&k)[HD / 16]) {
+  const size_t row = ((size_t)a.layer * it.P + key) * a.nkv + it.kvh;
+  if (!fp4) {
+    const bf16 *p = reinterpret_cast<const bf16 *>(it.pk) + row * HD + half * 8;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) k[i] = *reinterpret_cast<const bf16x8 *>(p + 16 * i);
+    return;
+  }
+  constexpr int NW = HD / 16, NB = HD >= 64 ? HD / 64 : 1;      // code words, blocks
+  const uint8_t *p = reinterpret_cast<const uint8_t *>(it.pk) + row * (HD / 2) + half * (HD / 4);
+  const uint8_t *sp = reinterpret_cast<const uint8_t *>(it.pk) + kv4_code_bytes(a.L, it.P, a.nkv, HD) + row * (HD / 32) +
+                      (HD >= 64 ? half * NB : 0);
+  uint32_t w[NW];
+  if constexpr (NW == 2) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(p);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < NW / 4; ++j) {
+      const uint4 v = reinterpret_cast<const uint4 *>(p)[j];
+      w[4 * j] = v.x; w[4 * j + 1] = v.y; w[4 * j + 2] = v.z; w[4 * j + 3] = v.w;
+    }
+  }
+  uint8_t s[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) s[j] = sp[j];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) k[i] = kv4_bf16x8(w[i], kv4_scale(s[i / 4]));
+}
+
+template <int HD, int KT, int WK>
+struct MassTile {
+  static constexpr int ROWB = HD * 2, CPR = ROWB / 16, TILEB = 32 * ROWB, NF = HD / 16;
+  static constexpr int WR = 4 / WK, KEYS = 32 * KT * WK;
+  static constexpr int STAGEB = WR * TILEB, UNITS = STAGEB / 1024;      // a stage of the ring: WR query tiles
+  static constexpr int DEPTH = 65536 / STAGEB < 4 ? 65536 / STAGEB : 4;
+  static constexpr int LSE = DEPTH * STAGEB;                            // then 64 lse words a stage and wave
+  static constexpr int LDSB = LSE + DEPTH * 4 * 256;
+  static_assert(DEPTH >= 2 && LDSB <= 81920, "two blocks a CU");
+};
+
+template <int HD, int KT, int WK, bool FP4>
+__global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
+  using T = MassTile<HD, KT, WK>;
+  constexpr int ROWB = T::ROWB, CPR = T::CPR, NF = T::NF, WR = T::WR, DEPTH = T::DEPTH;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDSB];
+  // Neighbouring items read the same queries: blocks of one XCD (every eighth) take a run of items.
+  const int per = a.n_items >> 3, b = blockIdx.x;
+  const MassItem it = a.items[b < 8 * per ? (b & 7) * per + (b >> 3) : b];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int col = lane & 31, half = lane >> 5, kg = wave % WK, rg = wave / WK;
+  const int G = a.nq / a.nkv, R = it.H * G, n = (R + 32 * WR - 1) / (32 * WR);
+  const float rG = 1.0f / (float)G;
+  const bf16 *qkv = reinterpret_cast<const bf16 *>(a.qkv);
+  const uint32_t lds0 = lds_u32(smem);
+
+  // The queries of stage t (rows past the last: the last one), whole rows side by side, chunk c of row r at
+  // c ^ swz(r), and the lse of the wave's own tile.  A row's token is its quotient by G, in fp32 exact below 2^20.
+  auto fetch = [&](int t) {
+    const int base = t * 32 * WR, tok0 = base / G, last = R - 1 - tok0 * G;
+    auto row_at = [&](int x, size_t &tok, int &head) {
+      x = min(base - tok0 * G + x, last);
+      const int q = (int)(((float)x + 0.5f) * rG);
+      tok = (size_t)(it.tok_off + tok0 + q);
+      head = it.kvh * G + x - q * G;
+    };
+    const uint32_t st = lds0 + (uint32_t)(t % DEPTH * T::STAGEB);
+    size_t tok;
+    int head;
+#pragma unroll
+    for (int j = 0; j < (T::UNITS + 3) / 4; ++j) {
+      const int u = wave + 4 * j;
+      if (T::UNITS % 4 && u >= T::UNITS) continue;
+      const int r = u * (64 / CPR) + lane / CPR, c = (lane % CPR) ^ at::swz(r, CPR);
+      row_at(r, tok, head);
+      dma_1k(qkv + tok * a.ldqkv + (size_t)head * HD + c * 8, st + u * 1024);
+    }
+    row_at(rg * 32 + col, tok, head);
+    dma_256(a.lse + tok * a.nq + head, lds0 + (uint32_t)(T::LSE + (t % DEPTH * 4 + wave) * 256));
+  };
+#pragma unroll
+  for (int t = 0; t < DEPTH - 1; ++t)
+    if (t < n) fetch(t);
+
+  const bool active = kg * KT * 32 < it.nk;
+  bf16x8 k[KT][NF];
+  if (active)
+#pragma unroll
+    for (int x = 0; x < KT; ++x) read_key<HD>(a, it, it.k0 + min((kg * KT + x) * 32 + col, it.nk - 1), half, FP4, k[x]);
+
+  const float sl2 = 1.4426950408889634f / sqrtf((float)HD);
+  float sum[KT] = {};
+  for (int t = 0; t < n; ++t) {
+    // stage t has landed (DEPTH - 2 behind it may not have: as many copies a wave, at least one); then it is in LDS
+    // for every wave, and every wave is done with stage t - 1, whose place the next takes
+    if (t + DEPTH - 1 > n || T::UNITS % 4) __builtin_amdgcn_s_waitcnt(at::waitcnt_vm(0));
+    else __builtin_amdgcn_s_waitcnt(at::waitcnt_vm((DEPTH - 2) * (T::UNITS / 4 + 1)));
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + DEPTH - 1 < n) fetch(t + DEPTH - 1);
+    const int base = (t * WR + rg) * 32;
+    if (!active || base >= R) continue;
+    const uint32_t q0 = lds0 + (uint32_t)(t % DEPTH * T::STAGEB + rg * T::TILEB + col * ROWB) +
+                        (uint32_t)(((FP4 ? NF * half : half) ^ at::swz(col, CPR)) << 4);
+    f32x16 s[KT] = {};
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const bf16x8 q = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds_ptr(q0 ^ (uint32_t)(i << (FP4 ? 4 : 5))));
+#pragma unroll
+      for (int x = 0; x < KT; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[x][i], s[x], 0, 0, 0);
+    }
+    // register r: query row (r / 4) 8 + 4 half + r % 4 of the tile
+    const uint32_t l0 = lds0 + (uint32_t)(T::LSE + (t % DEPTH * 4 + wave) * 256 + half * 16);
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const f32x4 l = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(lds_ptr(l0 + r4 * 32));
+#pragma unroll
+      for (int x = 0; x < KT; ++x) {
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = __builtin_amdgcn_exp2f(fmaf(s[x][4 * r4 + j], sl2, l[j] * -1.4426950408889634f));
+          if (base + 32 > R) w[j] = base + r4 * 8 + half * 4 + j < R ? w[j] : 0.f;
+        }
+        sum[x] += (w[0] + w[1]) + (w[2] + w[3]);
+      }
+    }
+  }
+  float *m = it.mass + ((size_t)a.layer * a.nkv + it.kvh) * it.P + it.k0;
+#pragma unroll
+  for (int x = 0; x < KT; ++x) sum[x] += __shfl_xor(sum[x], 32, 64);
+  if constexpr (WR > 1) {                       // the query groups' sums, in order
+    float *red = reinterpret_cast<float *>(smem);
+    __syncthreads();
+    if (half == 0)
+#pragma unroll
+      for (int x = 0; x < KT; ++x) red[rg * T::KEYS + (kg * KT + x) * 32 + col] = sum[x];
+    __syncthreads();
+    for (int j = threadIdx.x; j < it.nk; j += 256) {
+      float v = red[j];
+#pragma unroll
+      for (int r = 1; r < WR; ++r) v += red[r * T::KEYS + j];
+      m[j] = a.accumulate ? m[j] + v : v;
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const int j = (kg * KT + x) * 32 + col;
+      if (half == 0 && j < it.nk) m[j] = a.accumulate ? m[j] + sum[x] : sum[x];
+    }
+  }
+}
+
+template <int HD, int KT, int WK>
+static void launch_mass(const KvMassArgs &a, hipStream_t s) {
+  static_assert(MassTile<HD, KT, WK>::KEYS == kMassLarge || MassTile<HD, KT, WK>::KEYS == kMassSmall, "item sizes");
+  if (a.fp4) hipLaunchKernelGGL((kv_mass_kernel<HD, KT, WK, true>), dim3(a.n_items), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_mass_kernel<HD, KT, WK, false>), dim3(a.n_items), dim3(256), 0, s, a);
+}
+
+template <int HD>
+static hipError_t launch_mass_keys(const KvMassArgs &a, hipStream_t s) {
+  if (a.keys == kMassLarge) launch_mass<HD, 2, 4>(a, s);
+  else if (a.keys == kMassSmall) launch_mass<HD, 1, 2>(a, s);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+// Keys a block takes.  Large blocks read the queries from LDS once for two tiles of keys and from memory once for 256
+// keys; but a set of fewer than one of them for each CU is done sooner in small ones.
+int kv_mass_keys(bool bf16_mode, int64_t large_blocks) {
+  return !bf16_mode ? kMassRows : large_blocks >= 256 ? kMassLarge : kMassSmall;
+}
+
+hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
+  if (a.n_items <= 0) return hipSuccess;
+  if (!bf16_mode) return launch_kv_mass_rows(a, s);
+  switch (a.hd) {
+    case 32: return launch_mass_keys<32>(a, s);
+    case 64: return launch_mass_keys<64>(a, s);
+    case 128: return launch_mass_keys<128>(a, s);
+    case 256: return launch_mass_keys<256>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace rosa

@@ -664,6 +664,7 @@ int call_lanes(const rosa_capacity &cap, const rosa_request *reqs, int n, int ma
 // masses, the work of gathering them (items of plan requests [0, r] in upto[r]).
 struct KvUse {
   bool fp4 = false, gather = false;
+  int keys = 0;                     // of a mass item
   std::vector<MassItem> items;
   std::vector<int32_t> upto;
   bool plain() const { return !fp4 && !gather; }
@@ -779,6 +780,7 @@ hipError_t run_attention(rosa_batch *b, const Plan &p, const Plan::Lane &ln, int
     KvMassArgs ma{};
     ma.items = (const MassItem *)((uint8_t *)b->d_plan + b->off_mass) + m_lo;
     ma.n_items = m_hi - m_lo;
+    ma.keys = kv->keys;
     ma.layer = layer; ma.L = D.L;
     ma.qkv = qkv; ma.ldqkv = D.qkv_dim; ma.lse = b->lse;
     ma.nq = D.nq; ma.nkv = D.nkv; ma.hd = D.hd;
@@ -804,12 +806,15 @@ rosa_status plan_kv(rosa_batch *b, const Plan &p, const rosa_request *reqs, int 
   }
   if (!mass) return ROSA_OK;
   kv.upto.resize(n);
+  int64_t large = 0;
+  for (int i = 0; i < n; ++i) large += (int64_t)b->dims.nkv * ((reqs[i].prefix_len + kMassLarge - 1) / kMassLarge);
+  kv.keys = kv_mass_keys(b->bf16, large);
   for (int i = 0; i < n; ++i) {
     const rosa_request &r = reqs[p.order[i]];
     for (int kvh = 0; kvh < b->dims.nkv; ++kvh)
-      for (int k0 = 0; k0 < r.prefix_len; k0 += kMassKeys)
+      for (int k0 = 0; k0 < r.prefix_len; k0 += kv.keys)
         kv.items.push_back({r.prefix_k, mass[p.order[i]], r.prefix_len, r.horizon, p.tok_off[i], kvh, k0,
-                            std::min(kMassKeys, r.prefix_len - k0), {0, 0}});
+                            std::min(kv.keys, r.prefix_len - k0), {0, 0}});
     kv.upto[i] = (int32_t)kv.items.size();
   }
   return ROSA_OK;
@@ -1003,7 +1008,7 @@ rosa_status rosa_batch_create(const rosa_model_config *cfg, const rosa_weights *
     // many idle first entries (n_blocks <= items + 7)
     b->max_list_ints = (size_t)cap->max_steps * (2 * (size_t)b->max_items + 8 * kMaxLanes * n_sets);
     b->off_mass = align(b->off_lists + b->max_list_ints * sizeof(AttnItem));
-    b->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassKeys) + (size_t)cap->max_requests);
+    b->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassRows) + (size_t)cap->max_requests);
     b->plan_bytes = align(b->off_mass + b->max_mass * sizeof(MassItem));
     b->d_plan = dalloc<uint8_t>(b, b->plan_bytes, e);
     if (e != hipSuccess) {

@@ -322,7 +322,7 @@ hipError_t launch_kv4_merge(const AttnGroup *groups, int n_groups, const KvAttnA
 hipError_t launch_kv_attention(const KvAttnArgs &a, const AttnGroup *groups, int n_groups, bool bf16, hipStream_t s);
 
 // Keys [k0, k0 + nk) of one KV head of one request, whose attention weight
-// is summed over the request's H action tokens (nk <= kMassKeys).
+// is summed over the request's H action tokens (nk <= KvMassArgs::keys).
 struct MassItem {
   const void *pk;        // the request's K cache
   float *mass;           // [L][nkv][P]
@@ -330,15 +330,19 @@ struct MassItem {
   int32_t pad[2];
 };
 static_assert(sizeof(MassItem) == 48, "MassItem is 48 bytes");
-constexpr int kMassKeys = 32;
+constexpr int kMassRows = 32, kMassSmall = 64, kMassLarge = 256;   // keys an item: fp32 mode, bf16 mode
+// Keys an item of a call whose caches make large_blocks items of kMassLarge keys
+int kv_mass_keys(bool bf16, int64_t large_blocks);
 struct KvMassArgs {
   const MassItem *items; int n_items;
   int layer, L;
   const void *qkv; int ldqkv;
   const float *lse;      // [stacked row][nq]
   int nq, nkv, hd;
+  int keys;              // keys an item (at most)
   bool fp4, accumulate;
 };
 hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_kv_mass_rows(const KvMassArgs &a, hipStream_t s);      // fp32 mode
 
 }  // namespace rosa

@@ -33,7 +33,7 @@ struct rosa_kv {
     int list_at = 0, blocks = 0;                         // bf16: its launch list
     int groups = 0, group_base = 0;
   } sets[2];
-  int n_mass = 0;
+  int n_mass = 0, mass_keys = 0;
 
   // device plan region, two pinned staging copies
   uint8_t *d_plan = nullptr;
@@ -282,7 +282,7 @@ rosa_status rosa_kv_create(const rosa_model_config *cfg, const rosa_capacity *ca
     h->max_groups = (size_t)n_sets * kAttnMaxSlots;
     h->max_items = (size_t)n_sets * (kAttnMaxSlots + (size_t)blocks);
     h->max_lists = 2 * h->max_items + 8 * (size_t)n_sets;
-    h->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassKeys) + (size_t)cap->max_requests);
+    h->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassRows) + (size_t)cap->max_requests);
     auto align = [](size_t v) { return (v + 255) / 256 * 256; };
     h->off_items = 0;
     h->off_groups = align(h->off_items + (h->bf16 ? 0 : h->max_items) * sizeof(AttnItem));
@@ -344,12 +344,15 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     const Plan::AttnSet &S0 = p.sets[0], &S1 = p.sets[1];
     const size_t n_items = S0.items.size() + S1.items.size(), n_groups = S0.groups.size() + S1.groups.size();
     std::vector<MassItem> mi;
+    int64_t large = 0;
+    for (int i = 0; i < n; ++i) large += (int64_t)h->dims.nkv * ((rq[i].prefix_len + kMassLarge - 1) / kMassLarge);
+    const int keys = kv_mass_keys(h->bf16, large);
     if (mass)
       for (int i = 0; i < n; ++i)
         for (int kvh = 0; kvh < h->dims.nkv; ++kvh)
-          for (int k0 = 0; k0 < rq[i].prefix_len; k0 += kMassKeys)
+          for (int k0 = 0; k0 < rq[i].prefix_len; k0 += keys)
             mi.push_back({rq[i].prefix_k, mass[i], rq[i].prefix_len, rq[i].horizon, p.tok_off[i], kvh, k0,
-                          std::min(kMassKeys, rq[i].prefix_len - k0), {0, 0}});
+                          std::min(keys, rq[i].prefix_len - k0), {0, 0}});
     if (n_items > h->max_items || n_groups > h->max_groups || p.attn_lists.size() > h->max_lists || mi.size() > h->max_mass)
       return fail(h, ROSA_E_CAPACITY, "internal: plan above the handle's size");
 
@@ -397,6 +400,7 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     }
     h->n = n;
     h->n_mass = (int)mi.size();
+    h->mass_keys = keys;
     h->has_mass = mass != nullptr;
     h->fp4 = format == ROSA_KV_FP4;
     h->planned = true;
@@ -459,6 +463,7 @@ rosa_status rosa_kv_mass(rosa_kv *h, int32_t layer, const void *qkv, const float
     KvMassArgs a{};
     a.items = (const MassItem *)(h->d_plan + h->off_mass);
     a.n_items = h->n_mass;
+    a.keys = h->mass_keys;
     a.layer = layer; a.L = D.L;
     a.qkv = qkv; a.ldqkv = D.qkv_dim; a.lse = lse;
     a.nq = D.nq; a.nkv = D.nkv; a.hd = D.hd;
