@@ -6,21 +6,26 @@
 // cache's turned to bf16 there, exactly, once for all queries, so both formats share the products), and the
 // block's queries come by through a ring in LDS.  A block's waves take WK different groups of keys and 4 / WK
 // different tiles of queries; each key's sum is made by one block in a fixed order (no atomics).
-// 256 requests of 512 to 1280 cached tokens, 16 or 50 action tokens x 8 heads, head_dim 256: 66 us over
-// a bf16 cache (a key at a time on the vector units: 2220), 57 us over a 4-bit one; one request's 816
-// tokens under 50: 11 (385).  Bounds: the products take 14 us of the matrix cores, K 24 us (bf16) of HBM.
+// 256 requests of 512 to 1280 cached tokens, 16 or 50 action tokens x 8 heads, head_dim 256: 54 us over
+// a bf16 cache (a key at a time on the vector units: 2220), 45 us over a 4-bit one; one request's 816
+// tokens under 50: 9 (385).  Bounds: the products take 14 us of the matrix cores, K 24 us (bf16) of HBM.
 #include <math.h>
+
+#include <type_traits>
 
 #include "rosa_device.h"
 #include "rosa_internal.h"
 
 namespace rosa {
 
-// 64 floats, each lane's from its own address, to lds + 4 lane
-__device__ __forceinline__ void dma_256(const float *src, uint32_t lds) {
+// 64 floats, each lane's from its own byte offset behind a uniform base, to lds + 4 lane
+__device__ __forceinline__ void dma_256(const float *base, uint32_t off, uint32_t lds) {
+  const uint64_t b = (uint64_t)(size_t)base;
+  const uint64_t ub = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32) |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(ub), "s"(lds) : "memory", "m0");
 #pragma clang diagnostic pop
 }
 
@@ -84,28 +89,51 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
   const uint32_t lds0 = lds_u32(smem);
 
   // The queries of stage t (rows past the last: the last one), whole rows side by side, chunk c of row r at
-  // c ^ swz(r), and the lse of the wave's own tile.  A row's token is its quotient by G, in fp32 exact below 2^20.
-  auto fetch = [&](int t) {
-    const int base = t * 32 * WR, tok0 = base / G, last = R - 1 - tok0 * G;
-    auto row_at = [&](int x, size_t &tok, int &head) {
-      x = min(base - tok0 * G + x, last);
-      const int q = (int)(((float)x + 0.5f) * rG);
-      tok = (size_t)(it.tok_off + tok0 + q);
-      head = it.kvh * G + x - q * G;
-    };
-    const uint32_t st = lds0 + (uint32_t)(t % DEPTH * T::STAGEB);
-    size_t tok;
-    int head;
+  // c ^ swz(r), and the lse of the wave's own tile.  Row x of the stage: its token and head from their first
+  // ones (tok0, head0); a quotient by G in fp32, exact below 2^20.
+  constexpr int NU = (T::UNITS + 3) / 4;
+  auto row_of = [&](int x, int h0, int last, int &tok, int &head) {
+    x = min(h0 + x, last);
+    tok = (int)(((float)x + 0.5f) * rG);
+    head = x - tok * G;
+  };
+  auto unit_row = [&](int j) { return (wave + 4 * j) * (64 / CPR) + lane / CPR; };
+  auto unit_col = [&](int r) { return ((lane % CPR) ^ at::swz(r, CPR)) * 8; };
+  // Where G divides a stage its rows lie the same way in each: lane offsets made once.
+  const bool even = (32 * WR) % G == 0;
+  uint32_t qoff[NU], loff;
+  {
+    int tok, head;
 #pragma unroll
-    for (int j = 0; j < (T::UNITS + 3) / 4; ++j) {
-      const int u = wave + 4 * j;
-      if (T::UNITS % 4 && u >= T::UNITS) continue;
-      const int r = u * (64 / CPR) + lane / CPR, c = (lane % CPR) ^ at::swz(r, CPR);
-      row_at(r, tok, head);
-      dma_1k(qkv + tok * a.ldqkv + (size_t)head * HD + c * 8, st + u * 1024);
+    for (int j = 0; j < NU; ++j) {
+      row_of(unit_row(j), 0, 32 * WR, tok, head);
+      qoff[j] = (uint32_t)(tok * a.ldqkv + head * HD + unit_col(unit_row(j))) * 2;
     }
-    row_at(rg * 32 + col, tok, head);
-    dma_256(a.lse + tok * a.nq + head, lds0 + (uint32_t)(T::LSE + (t % DEPTH * 4 + wave) * 256));
+    row_of(rg * 32 + col, 0, 32 * WR, tok, head);
+    loff = (uint32_t)(tok * a.nq + head) * 4;
+  }
+  auto fetch = [&](int t) {
+    const int base = t * 32 * WR, tok0 = base / G;
+    const uint32_t st = lds0 + (uint32_t)(t % DEPTH * T::STAGEB), lst = lds0 + (uint32_t)(T::LSE + (t % DEPTH * 4 + wave) * 256);
+    const bf16 *q = qkv + (size_t)(it.tok_off + tok0) * a.ldqkv + (size_t)it.kvh * G * HD;
+    const float *l = a.lse + (size_t)(it.tok_off + tok0) * a.nq + it.kvh * G;
+    if (even && base + 32 * WR <= R) {
+#pragma unroll
+      for (int j = 0; j < NU; ++j)
+        if (T::UNITS % 4 == 0 || wave + 4 * j < T::UNITS) dma_1k_s(q, qoff[j], st + (wave + 4 * j) * 1024);
+      dma_256(l, loff, lst);
+      return;
+    }
+    const int h0 = base - tok0 * G, last = R - 1 - tok0 * G;
+    int tok, head;
+#pragma unroll
+    for (int j = 0; j < NU; ++j) {
+      if (T::UNITS % 4 && wave + 4 * j >= T::UNITS) continue;
+      row_of(unit_row(j), h0, last, tok, head);
+      dma_1k(q + (size_t)tok * a.ldqkv + head * HD + unit_col(unit_row(j)), st + (wave + 4 * j) * 1024);
+    }
+    row_of(rg * 32 + col, h0, last, tok, head);
+    dma_256(l, (uint32_t)(tok * a.nq + head) * 4, lst);
   };
 #pragma unroll
   for (int t = 0; t < DEPTH - 1; ++t)
@@ -116,6 +144,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
   if (active)
 #pragma unroll
     for (int x = 0; x < KT; ++x) read_key<HD>(a, it, it.k0 + min((kg * KT + x) * 32 + col, it.nk - 1), half, FP4, k[x]);
+  __builtin_amdgcn_s_waitcnt(at::waitcnt_vm(0));      // the keys, here: no wait for them is left to the loop
 
   const float sl2 = 1.4426950408889634f / sqrtf((float)HD);
   float sum[KT] = {};
@@ -130,29 +159,46 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
     if (!active || base >= R) continue;
     const uint32_t q0 = lds0 + (uint32_t)(t % DEPTH * T::STAGEB + rg * T::TILEB + col * ROWB) +
                         (uint32_t)(((FP4 ? NF * half : half) ^ at::swz(col, CPR)) << 4);
-    f32x16 s[KT] = {};
+    constexpr int RA = KT == 2 || NF < 6 ? (NF < 4 ? NF : 4) : 6;            // operands are read RA - 1 ahead
+    auto qfrag = [&](int i) {
+      return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds_ptr(q0 ^ (uint32_t)(i << (FP4 ? 4 : 5))));
+    };
+    bf16x8 q[RA];
 #pragma unroll
-    for (int i = 0; i < NF; ++i) {
-      const bf16x8 q = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds_ptr(q0 ^ (uint32_t)(i << (FP4 ? 4 : 5))));
-#pragma unroll
-      for (int x = 0; x < KT; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k[x][i], s[x], 0, 0, 0);
-    }
+    for (int i = 0; i < RA - 1; ++i) q[i] = qfrag(i);
     // register r: query row (r / 4) 8 + 4 half + r % 4 of the tile
     const uint32_t l0 = lds0 + (uint32_t)(T::LSE + (t % DEPTH * 4 + wave) * 256 + half * 16);
+    f32x4 l[4];
+    f32x16 s[KT] = {};
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const f32x4 l = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(lds_ptr(l0 + r4 * 32));
+    for (int i = 0; i < NF; ++i) {
+      if (i + RA - 1 < NF) q[(i + RA - 1) % RA] = qfrag(i + RA - 1);
+      else if (i + RA - 1 - NF < 4) l[i + RA - 1 - NF] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(lds_ptr(l0 + (i + RA - 1 - NF) * 32));
 #pragma unroll
-      for (int x = 0; x < KT; ++x) {
-        float w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] = __builtin_amdgcn_exp2f(fmaf(s[x][4 * r4 + j], sl2, l[j] * -1.4426950408889634f));
-          if (base + 32 > R) w[j] = base + r4 * 8 + half * 4 + j < R ? w[j] : 0.f;
-        }
-        sum[x] += (w[0] + w[1]) + (w[2] + w[3]);
-      }
+      for (int x = 0; x < KT; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[i % RA], k[x][i], s[x], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int j = RA - 1; j < 4; ++j) l[j] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(lds_ptr(l0 + j * 32));
+    auto add = [&](auto whole) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j4 = 0; j4 < 4; ++j4) {
+        const f32x4 lj = l[j4] * -1.4426950408889634f;
+#pragma unroll
+        for (int x = 0; x < KT; ++x) {
+          float w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] = __builtin_amdgcn_exp2f(fmaf(s[x][4 * j4 + j], sl2, lj[j]));
+            if (!whole.value) w[j] = base + j4 * 8 + half * 4 + j < R ? w[j] : 0.f;
+          }
+          sum[x] += (w[0] + w[1]) + (w[2] + w[3]);
+        }
+      }
+    };
+    if (base + 32 <= R) add(std::true_type{});
+    else add(std::false_type{});
   }
   float *m = it.mass + ((size_t)a.layer * a.nkv + it.kvh) * it.P + it.k0;
 #pragma unroll
