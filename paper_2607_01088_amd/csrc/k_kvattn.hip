@@ -65,6 +65,7 @@ struct Kv4Tile {
   static constexpr int AOFF = 2 * TILEB, KOFF = 4 * TILEB, RINGB = KOFF + 3 * K4TILE;
   static constexpr int STGB = 4 * NG * 32 * 2 * HD;        // output staging
   static constexpr int LDSB = RINGB > STGB ? RINGB : STGB;
+  static_assert(LDSB >= 4 * TILEB + 512, "a tile a wave and their sums");
   // chunk swizzle of code rows: the 16 rows that a 16-lane group reads at one chunk fall in
   // distinct 16-byte columns of the 256-byte bank row
   static constexpr int SHIFT = K4ROW == 128 ? 1 : K4ROW == 64 ? 2 : K4ROW == 32 ? 3 : 4;
@@ -118,6 +119,251 @@ __device__ __forceinline__ uint32_t split_query(const bf16x8 (&q)[4], u32x6 (&t)
   return a >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
 }
 
+// ------------------------------------------------------------------ few rows
+// An item of at most 16 query rows (an action token or two): memory and latency are all it costs, so its four
+// waves take different keys, tile by tile in turn, with no barrier between them.  16 x 16 tiles, a
+// lane one query row (lane & 15): S^T = K Q^T with 128-wide products of codes that come straight from the cache
+// into registers (lane group g, lane >> 4: block 4 c + g of keys lane & 15 and 16 more), O^T += V^T P^T with V
+// turned to bf16 through a tile of LDS that is the wave's own.  The loads of a wave's next tile or
+// two are always on their way; the waves' O are joined in order at the end.
+constexpr int kFewRows = 16;
+
+template <int HD>
+__device__ __forceinline__ void kv4_few_rows(const KvAttnArgs &ka, const AttnItem &it, uint8_t *smem, float sl2) {
+  constexpr int ROWB = HD * 2, CPR = ROWB / 16, TILEB = 32 * ROWB, K4ROW = HD / 2, CK = HD / 32;
+  constexpr int NP = HD > 128 ? HD / 128 : 1;              // 128-wide products
+  constexpr int NB = CK > 2 ? CK / 2 : 1;                  // V blocks a lane turns to bf16
+  constexpr int NT = HD / 16;
+  const AttnArgs &a = ka.a;
+  const int G = a.nq / a.nkv;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, r = lane & 15, g = lane >> 4;
+  const uint32_t lds0 = lds_u32(smem), tile0 = lds0 + (uint32_t)(wave * TILEB);
+  const __attribute__((address_space(1))) bf16 *qkv = (const __attribute__((address_space(1))) bf16 *)(a.qkv);
+
+  const int x = it.q0 + min(r, it.nq - 1), head = it.kvh * G + x % G;
+  const size_t tok = (size_t)(it.tok_off + x / G);
+  const __attribute__((address_space(1))) bf16 *qp = qkv + tok * a.ldqkv + (size_t)head * HD;
+  const int pn = max(0, min(it.kend, it.P) - it.kbeg), np = (pn + 31) >> 5;
+  const int ab = max(it.kbeg, it.P), an = max(0, it.kend - ab), na = (an + 31) >> 5;
+
+  f32x4 o[NT];
+  float mb = 3e38f, l = 0.f;                               // as in the kernel below
+#pragma unroll
+  for (int n = 0; n < NT; ++n) o[n] = f32x4{};
+
+  // Rows of V in LDS: chunk c of row k at c ^ swz(k).  The transposed reads: rows 4 g + (lane & 15) / 4 and 16
+  // more, 8 bytes each of a tile's 32.
+  uint32_t vbase;
+  {
+    const int k = 4 * g + (r >> 2);
+    vbase = tile0 + (uint32_t)(k * ROWB + ((((r >> 1) & 1) ^ at::swz(k, CPR)) << 4) + 8 * (r & 1));
+  }
+  // Scores (s[h] register j: key 16 h + 4 g + j, masked from n_keys on) to weights, and their V rows, which are
+  // in LDS, onto O.
+  auto accumulate = [&](f32x4 (&s)[2], int n_keys) __attribute__((always_inline)) {
+    if (n_keys < 32) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (16 * h + 4 * g + j >= n_keys) s[h][j] = -INFINITY;
+    }
+    float tmax = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) tmax = fmaxf(tmax, s[i / 4][i % 4]);
+    if (__ballot(fmaf(tmax, sl2, mb) > 32.0f)) {
+      float tm = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
+      tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
+      const bool up = fmaf(tm, sl2, mb) > 32.0f;           // the groups of a query agree
+      const float nb = up ? -tm * sl2 : mb, f = up ? __builtin_amdgcn_exp2f(nb - mb) : 1.0f;
+      mb = nb;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[n] *= f;
+    }
+    asm volatile("" ::: "memory");                         // V rows written, then read (LDS keeps a wave's order)
+    bf16x8 p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], sl2, mb));
+      l += w;
+      p[i] = (bf16)w;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint32_t v = vbase ^ (uint32_t)(n << 5);
+      o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_tr_pair(lds_ptr(v), lds_ptr(v) + 16 * ROWB), p, o[n], 0, 0, 0);
+    }
+  };
+
+  if (wave < np) {
+    u32x6 q6[NP][3];
+    uint32_t qs[NP];
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+      const int b = 4 * c + g;
+      bf16x8 q[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        q[j] = *(const __attribute__((address_space(1))) bf16x8 *)(qp + 32 * (b < CK ? b : 0) + 8 * j);
+        if (b >= CK) q[j] = bf16x8{};                      // a product is 128 wide
+      }
+      qs[c] = split_query(q, q6[c]);
+    }
+    // A tile: codes and scales of its keys, and of the V blocks that this lane turns to bf16 (rows and blocks dealt
+    // so that 16 lanes write distinct 16-byte columns)
+    auto vblock = [&](int j, int &row, int &blk) __attribute__((always_inline)) {
+      if constexpr (HD == 256) { blk = (lane & 3) | ((lane >> 2) & 4); row = (((lane >> 2) & 3) << 2) | (lane >> 5) | ((j & 1) << 1) | ((j >> 1) << 4); }
+      else if constexpr (HD == 128) { blk = lane & 3; row = (((lane >> 2) & 3) << 2) | (lane >> 4) | (j << 4); }
+      else { blk = lane % CK; row = (lane / CK) & 31; }
+    };
+    const uint32_t rowb = (uint32_t)a.nkv * K4ROW, srow = (uint32_t)a.nkv * CK;
+    const size_t r0 = ((size_t)a.layer * it.P + it.kbeg) * a.nkv + it.kvh, codes = kv4_code_bytes(ka.L, it.P, a.nkv, HD);
+    typedef const __attribute__((address_space(1))) uint8_t g_u8;
+    g_u8 *pk = (g_u8 *)(size_t)it.pk, *pv = (g_u8 *)(size_t)it.pv;
+    struct Tile {
+      i32x4 k[2][NP], v[NB];
+      uint32_t ks[2][NP], vs[NB];
+    };
+    auto load = [&](Tile &x, int f) __attribute__((always_inline)) {
+      g_u8 *kc = pk + (r0 + (size_t)f * a.nkv) * K4ROW, *vc = pv + (r0 + (size_t)f * a.nkv) * K4ROW;
+      g_u8 *kz = pk + codes + (r0 + (size_t)f * a.nkv) * CK, *vz = pv + codes + (r0 + (size_t)f * a.nkv) * CK;
+      const int last = pn - 1 - f;                         // rows past the last: the last one
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+          const uint32_t row = (uint32_t)min(16 * h + r, last), b = (uint32_t)(4 * c + g < CK ? 4 * c + g : 0);
+          x.k[h][c] = *(const __attribute__((address_space(1))) i32x4 *)(kc + (row * rowb + b * 16));
+          x.ks[h][c] = kz[row * srow + b];
+        }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        int row, blk;
+        vblock(j, row, blk);
+        row = min(row, last);
+        x.v[j] = *(const __attribute__((address_space(1))) i32x4 *)(vc + ((uint32_t)row * rowb + (uint32_t)blk * 16));
+        x.vs[j] = vz[(uint32_t)row * srow + (uint32_t)blk];
+      }
+    };
+    // tile t, which x holds; then the wave's DEEP-next tile leaves for x (past the last tile that one again).
+    // Two tiles on their way at head_dim 256 take registers that the other items' key loop, in the same kernel, needs.
+    constexpr int DEEP = HD == 256 ? 1 : 2;
+    auto step = [&](Tile &x, int t) __attribute__((always_inline)) {
+      f32x4 s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[h] = f32x4{};
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+          i32x4 kk = x.k[h][c];
+          if (CK < 4 && g >= CK) kk = i32x4{};
+          const i32x8 kf = __builtin_shufflevector(kk, kk, 0, 1, 2, 3, -1, -1, -1, -1);
+#pragma unroll
+          for (int x3 = 0; x3 < 3; ++x3) {
+            const i32x6 q = __builtin_bit_cast(i32x6, q6[c][x3]);
+            const i32x8 qf = __builtin_shufflevector(q, q, 0, 1, 2, 3, 4, 5, -1, -1);
+            s[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, qf, s[h], 4, 2, 0, x.ks[h][c], 0, qs[c] - (x3 == 0 ? 0 : x3 == 1 ? 4 : 9));
+          }
+        }
+      }
+      if (32 * CK >= 64 || lane < 32 * CK)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          int row, blk;
+          vblock(j, row, blk);
+          const uint32_t d = tile0 + (uint32_t)(row * ROWB + (((4 * blk) ^ at::swz(row, CPR)) << 4));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<__attribute__((address_space(3))) bf16x8 *>((__attribute__((address_space(3))) uint8_t *)(size_t)(d ^ (i << 4))) =
+                kv4_bf16x8((uint32_t)x.v[j][i], kv4_scale((uint8_t)x.vs[j]));
+        }
+      load(x, 32 * min(t + 4 * DEEP, np - 1));
+      accumulate(s, pn - 32 * t);
+    };
+    Tile x0;
+    load(x0, 32 * wave);
+    int t = wave;
+    if constexpr (DEEP == 1) {
+      for (; t < np; t += 4) step(x0, t);
+    } else {
+      Tile x1;
+      load(x1, 32 * min(wave + 4, np - 1));
+      const int cnt = (np - wave + 3) >> 2;
+      for (int i = 0; i < cnt >> 1; ++i, t += 8) {         // (no exit between the steps: the compiler would wait for both tiles)
+        step(x0, t);
+        step(x1, t + 4);
+      }
+      if (cnt & 1) step(x0, t);
+    }
+  }
+  // the request's own keys, tiles np, np + 1, .. of the item
+  for (int u = (wave - np) & 3; u < na; u += 4) {
+    const int last = an - 1 - 32 * u;
+    const __attribute__((address_space(1))) bf16 *ap = qkv + (size_t)(it.tok_off + ab - it.P + 32 * u) * a.ldqkv;
+    const int kcol = (a.nq + it.kvh) * HD, vcol = (a.nq + a.nkv + it.kvh) * HD;
+    f32x4 s[2] = {};
+#pragma unroll
+    for (int c = 0; c < HD / 32; ++c) {
+      const bf16x8 q = *(const __attribute__((address_space(1))) bf16x8 *)(qp + 32 * c + 8 * g);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 kf = *(const __attribute__((address_space(1))) bf16x8 *)(ap + (size_t)min(16 * h + r, last) * a.ldqkv + kcol + 32 * c + 8 * g);
+        s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q, s[h], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 32 * CPR / 64; ++i) {
+      const int row = (i * 64 + lane) / CPR, c = lane % CPR;
+      const i32x4 w = *(const __attribute__((address_space(1))) i32x4 *)(ap + (size_t)min(row, last) * a.ldqkv + vcol + c * 8);
+      *reinterpret_cast<__attribute__((address_space(3))) i32x4 *>((__attribute__((address_space(3))) uint8_t *)(size_t)(tile0 + row * ROWB + ((c ^ at::swz(row, CPR)) << 4))) = w;
+    }
+    accumulate(s, last + 1);
+  }
+
+  // ---- the waves' results through LDS: o[n] as it lies, reference and sum behind them
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  lds_barrier();
+  f32x4 *so = reinterpret_cast<f32x4 *>(smem);
+  float2 *sml = reinterpret_cast<float2 *>(smem + 4 * TILEB);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) so[(wave * NT + n) * 64 + lane] = o[n];
+  if (g == 0) sml[wave * 16 + r] = make_float2(-mb, l);
+  __syncthreads();
+  float m = sml[r].x, f[4], L = 0.f;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m = fmaxf(m, sml[w * 16 + r].x);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = exp2f(sml[w * 16 + r].x - m);
+    L += f[w] * sml[w * 16 + r].y;
+  }
+  if (r < it.nq) {
+    const float inv = 1.0f / L;
+    for (int n = wave; n < NT; n += 4) {
+      f32x4 y = {};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) y += so[(w * NT + n) * 64 + lane] * f[w];
+      const int col = 16 * n + 4 * g;
+      if (it.slot >= 0) {
+        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.part_o) + ((size_t)it.slot * kAttnQB + r) * HD + col) = y;
+      } else {
+        const size_t oc = (size_t)head * HD + col;
+        const bf16x4 b = {(bf16)(y[0] * inv), (bf16)(y[1] * inv), (bf16)(y[2] * inv), (bf16)(y[3] * inv)};
+        *reinterpret_cast<bf16x4 *>(reinterpret_cast<bf16 *>(a.o) + (a.o_rows > 0 ? kb32_offset(a.o_rows, tok, oc) : tok * a.ldo + oc)) = b;
+      }
+    }
+    if (wave == 0 && g == 0) {
+      if (it.slot >= 0) *reinterpret_cast<float2 *>(a.part_ml + ((size_t)it.slot * kAttnQB + r) * 2) = make_float2(m, L);
+      else if (a.lse) a.lse[tok * a.nq + head] = (m + log2f(L)) * 0.6931471805599453f;
+    }
+  }
+  lds_barrier();
+}
+
 template <int HD, int NG>
 __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
   using T = Kv4Tile<HD, NG>;
@@ -140,6 +386,10 @@ __global__ void __launch_bounds__(256, 2) kv4_attention_kernel(KvAttnArgs ka) {
     __builtin_memcpy(&it, w, sizeof(AttnItem));
   }
   e = it.next;
+  if (it.nq <= kFewRows) {
+    kv4_few_rows<HD>(ka, it, smem, sl2);
+    continue;
+  }
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));      // per-lane addresses are not kept across items
   const int lane = tid & 63, half = lane >> 5;
@@ -603,39 +853,54 @@ hipError_t launch_kv4_attention(const KvAttnArgs &ka, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ joining split items
-// One wave per query row: o = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c, slots in
-// order.  Lane holds head-dim elements 4 lane ..
+// o = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c over a group's slots c, a wave a query row, slots in
+// order, eight in flight.  A group of few rows has many slots (one long request: 64): there a block's waves take
+// every fourth slot of one row and are joined in order.  Lane holds head-dim elements 4 lane ..
 __global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restrict__ groups, KvAttnArgs ka) {
+  __shared__ float sacc[4][64][4], sml[4];
   const AttnArgs &a = ka.a;
   const AttnGroup gr = groups[blockIdx.y];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int qloc = blockIdx.x * 4 + wave, G = a.nq / a.nkv, hd = a.hd;
+  const int nw = gr.nq <= kAttnQB / 4 ? 4 : 1;             // waves a row
+  const int qloc = nw == 4 ? blockIdx.x : blockIdx.x * 4 + wave, G = a.nq / a.nkv, hd = a.hd;
   if (qloc >= gr.nq) return;
   const bool on = 4 * lane < hd;
   const float *po = reinterpret_cast<const float *>(a.part_o);
   const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
-  // a lane's share of the slots' maxima and sums
+  // a lane's share of the slots' maxima
   float mx = -INFINITY;
   for (int c = lane; c < gr.n; c += 64) mx = fmaxf(mx, ml[(size_t)(gr.first_slot + c) * kAttnQB + qloc].x);
   mx = wave_max(mx);
   constexpr int CH = 8;
   float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int c0 = 0; c0 < gr.n; c0 += CH) {
+  for (int c0 = nw == 4 ? wave : 0; c0 < gr.n; c0 += nw * CH) {
     float2 p[CH];
     float4 v[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const bool live = c0 + c < gr.n;
-      const size_t r = (size_t)(gr.first_slot + (live ? c0 + c : 0)) * kAttnQB + qloc;
+      const bool live = c0 + nw * c < gr.n;
+      const size_t r = (size_t)(gr.first_slot + (live ? c0 + nw * c : 0)) * kAttnQB + qloc;
       p[c] = live ? ml[r] : make_float2(-INFINITY, 0.f);
       v[c] = live && on ? *reinterpret_cast<const float4 *>(po + r * hd + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const float w = exp2f(p[c].x - mx);
-      if (c0 + c >= gr.n) break;
+      if (c0 + nw * c >= gr.n) break;
       L += w * p[c].y;
       acc[0] += w * v[c].x; acc[1] += w * v[c].y; acc[2] += w * v[c].z; acc[3] += w * v[c].w;
+    }
+  }
+  if (nw == 4) {                                           // the whole block
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sacc[wave][lane][j] = acc[j];
+    if (lane == 0) sml[wave] = L;
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < 4; ++w) {
+      L += sml[w];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] += sacc[w][lane][j];
     }
   }
   const int qrow = gr.q0 + qloc;
