@@ -121,12 +121,16 @@ __device__ __forceinline__ uint32_t mass_key(float m) {
 // One block per (layer, KV head) row of a job: the `want` = keep - first - last
 // largest of its unprotected masses.  Four passes over the row find the key T of
 // the want-th largest, eight bits at a time (histogram of the keys that share
-// the bits found so far); a last pass lists the protected tokens, the keys above T
-// and the first ties at T, in order.
-__global__ void __launch_bounds__(256) kv_select_kernel(KvEvictJobs jobs, int rows) {
+// the bits found so far; the digit by a sum over the larger ones across the block); a last pass lists the
+// protected tokens, the keys above T and the first ties at T, in order.  The row is read from memory once,
+// but for what lies behind its first kSelectRow tokens.  Latency bounds it: 18 rows of 816 tokens take
+// 9 us, 576 of 512 to 1280 tokens 14.
+constexpr int kSelectRow = 12288;
+__global__ void __launch_bounds__(1024) kv_select_kernel(KvEvictJobs jobs, int rows) {
   __shared__ uint32_t hist[256];
   __shared__ uint32_t sh[2];
-  __shared__ uint32_t wsum[2][4];
+  __shared__ uint32_t wsum[2][16];
+  extern __shared__ float near[];            // the row's first kSelectRow masses
   const KvEvictJob &j = jobs.j[blockIdx.y];
   const int row = blockIdx.x, P = j.P, keep = j.keep;
   if (keep == 0) return;
@@ -135,68 +139,90 @@ __global__ void __launch_bounds__(256) kv_select_kernel(KvEvictJobs jobs, int ro
   float *kmass = j.kept_mass ? j.kept_mass + (size_t)row * keep : nullptr;
   const int lo = j.first, hi = P - j.last;
   const uint32_t want = (uint32_t)(keep - j.first - j.last);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nt = blockDim.x, nw = nt >> 6;
+  for (int i = tid; i < min(P, kSelectRow); i += nt) near[i] = mass[i];
+  __syncthreads();
+  auto at_row = [&](int i) { return i < kSelectRow ? near[i] : mass[i]; };
   uint32_t T = 0, left = want;               // bits found; how many of the keys that share them are wanted
   if (want > 0)
     for (int shift = 24; shift >= 0; shift -= 8) {
-      hist[tid] = 0;
+      if (tid < 256) hist[tid] = 0;
       __syncthreads();
       const uint32_t above = shift == 24 ? 0u : ~0u << (shift + 8);
-      for (int i = lo + tid; i < hi; i += 256) {
-        const uint32_t k = mass_key(mass[i]);
-        if ((k & above) == T) atomicAdd(&hist[(k >> shift) & 255], 1u);
+      for (int i0 = lo + tid; i0 < hi; i0 += 4 * nt) {
+        uint32_t k[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) k[x] = mass_key(at_row(min(i0 + x * nt, hi - 1)));
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (i0 + x * nt < hi && (k[x] & above) == T) atomicAdd(&hist[(k[x] >> shift) & 255], 1u);
       }
       __syncthreads();
-      if (tid == 0) {
-        uint32_t acc = 0;
-        int d = 255;
-        for (; d > 0; --d) {
-          if (acc + hist[d] >= left) break;
-          acc += hist[d];
-        }
-        sh[0] = T | (uint32_t)d << shift;
-        sh[1] = left - acc;
+      // thread d: the keys of digits d and above; exactly one d has `left` of them but not above it
+      const uint32_t own = tid < 256 ? hist[tid] : 0;
+      uint32_t sum = own;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_down(sum, o, 64);
+        if (lane + o < 64) sum += v;
+      }
+      if (lane == 0) wsum[0][wave] = sum;
+      __syncthreads();
+      for (int w = wave + 1; w < 4; ++w) sum += wsum[0][w];
+      if (tid < 256 && sum >= left && sum - own < left) {
+        sh[0] = T | (uint32_t)tid << shift;
+        sh[1] = left - (sum - own);
       }
       __syncthreads();
       T = sh[0];
       left = sh[1];
       __syncthreads();
     }
-  // `left` of the keys equal to T are kept: those of the lowest indices
-  uint32_t ties = 0, out = 0;                // so far, over the whole block
-  for (int i0 = 0; i0 < P; i0 += 256) {
-    const int i = i0 + tid;
-    const float m = i < P ? mass[i] : 0.f;
-    const bool safe = i < P && (i < lo || i >= hi);
+  // `left` of the keys equal to T are kept: those of the lowest indices.  A wave takes a run of the row: it
+  // counts, and with the runs before it counted it knows where its own tokens go.
+  const int run = ((P + nw - 1) / nw + 63) & ~63, r0 = wave * run, r1 = min(P, r0 + run);
+  auto look = [&](int i, float &m, bool &sure, bool &tie) {
+    m = at_row(min(i, P - 1));
     const uint32_t k = mass_key(m);
-    const bool cand = i < P && !safe && want > 0;
-    const bool tie = cand && k == T;
-    const uint64_t tb = __ballot(tie), below = (1ull << lane) - 1;
-    if (lane == 0) wsum[0][wave] = (uint32_t)__popcll(tb);
-    __syncthreads();
-    uint32_t trank = ties + (uint32_t)__popcll(tb & below);
-    uint32_t tall = ties;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) trank += wsum[0][w];
-      tall += wsum[0][w];
+    const bool safe = i < lo || i >= hi, cand = !safe && want > 0;
+    sure = i < r1 && (safe || (cand && k > T));
+    tie = i < r1 && cand && k == T;
+  };
+  uint32_t ties = 0, out = 0;
+  for (int i0 = r0; i0 < r1; i0 += 256) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float m;
+      bool sure, tie;
+      look(i0 + 64 * x + lane, m, sure, tie);
+      out += (uint32_t)__popcll(__ballot(sure));
+      ties += (uint32_t)__popcll(__ballot(tie));
     }
-    const bool take = safe || (cand && (k > T || (tie && trank < left)));
-    const uint64_t kb = __ballot(take);
-    if (lane == 0) wsum[1][wave] = (uint32_t)__popcll(kb);
-    __syncthreads();
-    uint32_t at = out + (uint32_t)__popcll(kb & below);
-    uint32_t oall = out;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) at += wsum[1][w];
-      oall += wsum[1][w];
+  }
+  if (lane == 0) { wsum[0][wave] = ties; wsum[1][wave] = out; }
+  __syncthreads();
+  ties = out = 0;
+  for (int w = 0; w < wave; ++w) { ties += wsum[0][w]; out += wsum[1][w]; }
+  out += min(ties, left);
+  const uint64_t below = (1ull << lane) - 1;
+  for (int i0 = r0; i0 < r1; i0 += 256) {
+    float m[4];
+    bool sure[4], tie[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) look(i0 + 64 * x + lane, m[x], sure[x], tie[x]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const uint64_t tb = __ballot(tie[x]);
+      const bool take = sure[x] || (tie[x] && ties + (uint32_t)__popcll(tb & below) < left);
+      const uint64_t kb = __ballot(take);
+      if (take) {
+        const uint32_t at = out + (uint32_t)__popcll(kb & below);
+        kept[at] = i0 + 64 * x + lane;
+        if (kmass) kmass[at] = m[x];
+      }
+      ties += (uint32_t)__popcll(tb);
+      out += (uint32_t)__popcll(kb);
     }
-    if (take) {
-      kept[at] = i;
-      if (kmass) kmass[at] = m;
-    }
-    ties = tall;
-    out = oall;
-    __syncthreads();
   }
 }
 
@@ -240,7 +266,13 @@ hipError_t launch_kv_evict(const KvEvictJobs &jobs, int n, int L, int nkv, int h
   int most = 0;
   for (int i = 0; i < n; ++i) most = std::max(most, jobs.j[i].keep);
   if (n <= 0 || most == 0) return hipSuccess;
-  hipLaunchKernelGGL(kv_select_kernel, dim3(L * nkv, n), dim3(256), 0, s, jobs, L * nkv);
+  int longest = 0;
+  for (int i = 0; i < n; ++i) longest = std::max(longest, jobs.j[i].P);
+  // Rows of few tokens want many blocks a CU, long ones many loads in flight a row: 256 and 1024 threads take
+  // 14 and 20 us over 576 rows of 512 to 1280 tokens, 637 and 287 over 4 rows of 131072 (the latter before the last pass was
+  // dealt to the waves in runs: 178 now).
+  hipLaunchKernelGGL(kv_select_kernel, dim3(L * nkv, n), dim3(longest <= 4096 ? 256 : 1024),
+                     std::min(longest, kSelectRow) * sizeof(float), s, jobs, L * nkv);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int pieces = (fp4 ? hd / 2 : hd * esz) / 16;
