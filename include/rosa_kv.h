@@ -95,7 +95,7 @@ typedef struct rosa_kv_evict_job {
 } rosa_kv_evict_job;
 
 /* Evict n requests' tokens from caches in `format`.  Deterministic, no memory, two
- * launches per 32 jobs; capturable.  Nothing that is written may overlap
+ * launches per 32 jobs (three of 4-bit caches); capturable.  Nothing that is written may overlap
  * anything else the call reads or writes (so not in place).  Errors as
  * rosa_kv_quantize. */
 rosa_status rosa_kv_evict(const rosa_model_config *cfg, int32_t format, const rosa_kv_evict_job *jobs, int32_t n,
@@ -117,7 +117,8 @@ rosa_status rosa_kv_create(const rosa_model_config *cfg, const rosa_capacity *ca
 /* Plan the attention of a request set, for every layer: prefix_k / prefix_v /
  * prefix_len / horizon of each request are read (the caches in `format`), the other
  * fields ignored.  mass: NULL, or a HOST array of n DEVICE pointers, each the
- * request's masses [L][n_kv][P] fp32 (NULL where P is 0).  The plan is copied to the
+ * request's masses [L][n_kv][P] fp32 (NULL where P is 0), apart from each other and from the
+ * caches (which requests may share).  The plan is copied to the
  * device on the handle's stream and replaces the last one; the arrays it names
  * must stay valid while calls use it.  Not under graph capture
  * (ROSA_E_INVALID); the calls below may be captured once a plan is there, and the graph

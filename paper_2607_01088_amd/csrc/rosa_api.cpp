@@ -801,10 +801,13 @@ rosa_status plan_kv(rosa_batch *b, const Plan &p, const rosa_request *reqs, int 
   for (int i = 0; i < n; ++i) {
     if (((uintptr_t)reqs[i].prefix_k | (uintptr_t)reqs[i].prefix_v) & 15)
       return fail(b, ROSA_E_INVALID, "a prefix cache is not 16-byte aligned");
-    if (mass && reqs[i].prefix_len > 0 && (!mass[i] || (uintptr_t)mass[i] & 3))
-      return fail(b, ROSA_E_INVALID, "a request's masses are NULL or not 4-byte aligned");
   }
   if (!mass) return ROSA_OK;
+  const int32_t format = kv.fp4 ? ROSA_KV_FP4 : ROSA_KV_MODEL;
+  if (const char *why = masses_unusable(reqs, n, mass, (size_t)b->dims.L * b->dims.nkv, [&](const rosa_request &r) {
+        return (size_t)rosa_kv_bytes(&b->cfg, format, r.prefix_len);
+      }))
+    return fail(b, ROSA_E_INVALID, why);
   kv.upto.resize(n);
   int64_t large = 0;
   for (int i = 0; i < n; ++i) large += (int64_t)b->dims.nkv * ((reqs[i].prefix_len + kMassLarge - 1) / kMassLarge);

@@ -88,23 +88,6 @@ size_t fp4_bytes(const rosa_model_config *c, int64_t P) {
   return kv4_bytes((size_t)c->n_layers, (size_t)P, (size_t)c->n_kv_heads, (size_t)c->head_dim);
 }
 
-// Address ranges of a call: whether a written one overlaps any other.
-struct Range { uintptr_t lo, hi; bool written; };
-bool clash(std::vector<Range> &r) {
-  std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
-  uintptr_t any = 0, written = 0;              // ends of the ranges so far
-  for (const Range &x : r) {
-    if (x.lo == x.hi) continue;
-    if (x.lo < written || (x.written && x.lo < any)) return true;
-    any = std::max(any, x.hi);
-    if (x.written) written = std::max(written, x.hi);
-  }
-  return false;
-}
-void add_range(std::vector<Range> &r, const void *p, size_t bytes, bool written) {
-  if (p && bytes) r.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written});
-}
-
 rosa_status check_cfg(const rosa_model_config *cfg) {
   if (!cfg) return fail(nullptr, ROSA_E_INVALID, "cfg is NULL");
   const rosa_status st = check_config(cfg);
@@ -338,9 +321,12 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     for (int i = 0; i < n; ++i) {
       if (!aligned(rq[i].prefix_k, 16) || !aligned(rq[i].prefix_v, 16))
         return fail(h, ROSA_E_INVALID, "a prefix cache is not 16-byte aligned");
-      if (mass && rq[i].prefix_len > 0 && (!mass[i] || !aligned(mass[i], 4)))
-        return fail(h, ROSA_E_INVALID, "a request's masses are NULL or not 4-byte aligned");
     }
+    if (mass)
+      if (const char *why = masses_unusable(rq.data(), n, mass, (size_t)h->dims.L * h->dims.nkv, [&](const rosa_request &r) {
+            return (size_t)rosa_kv_bytes(&h->cfg, format, r.prefix_len);
+          }))
+        return fail(h, ROSA_E_INVALID, why);
     const Plan::AttnSet &S0 = p.sets[0], &S1 = p.sets[1];
     const size_t n_items = S0.items.size() + S1.items.size(), n_groups = S0.groups.size() + S1.groups.size();
     std::vector<MassItem> mi;

@@ -4,6 +4,7 @@
 
 #include <stdint.h>
 
+#include <algorithm>
 #include <string>
 #include <vector>
 
@@ -52,6 +53,37 @@ struct Plan {
   // idle block) and each entry's link to its block's next entry.
   std::vector<int32_t> attn_lists, attn_next;
 };
+
+// Address ranges of a call: whether a written one overlaps any other.
+struct Range { uintptr_t lo, hi; bool written; };
+inline bool clash(std::vector<Range> &r) {
+  std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
+  uintptr_t any = 0, written = 0;              // ends of the ranges so far
+  for (const Range &x : r) {
+    if (x.lo == x.hi) continue;
+    if (x.lo < written || (x.written && x.lo < any)) return true;
+    any = std::max(any, x.hi);
+    if (x.written) written = std::max(written, x.hi);
+  }
+  return false;
+}
+inline void add_range(std::vector<Range> &r, const void *p, size_t bytes, bool written) {
+  if (p && bytes) r.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written});
+}
+// Masses of a request set over caches of cache_bytes(request) bytes: usable, and apart from each other and from
+// the caches (requests may share caches, but each token's mass is one block's to write).
+template <typename Bytes>
+const char *masses_unusable(const rosa_request *reqs, int n, float *const *mass, size_t rows, Bytes cache_bytes) {
+  std::vector<Range> ranges;
+  for (int i = 0; i < n; ++i) {
+    if (reqs[i].prefix_len <= 0) continue;
+    if (!mass[i] || (uintptr_t)mass[i] & 3) return "a request's masses are NULL or not 4-byte aligned";
+    add_range(ranges, reqs[i].prefix_k, cache_bytes(reqs[i]), false);
+    add_range(ranges, reqs[i].prefix_v, cache_bytes(reqs[i]), false);
+    add_range(ranges, mass[i], rows * reqs[i].prefix_len * 4, true);
+  }
+  return clash(ranges) ? "a request's masses overlap another array of the call" : nullptr;
+}
 
 rosa_status check_config(const rosa_model_config *c);
 rosa_status check_capacity(const rosa_capacity *c);
