@@ -864,24 +864,31 @@ hipError_t launch_kv4_attention(const KvAttnArgs &ka, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ joining split items
-// o = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c over a group's slots c, a wave a query row, slots in
-// order, eight in flight.  A group of few rows has many slots (one long request: 64): there a block's waves take
-// every fourth slot of one row and are joined in order.  Lane holds head-dim elements 4 lane ..
+// o = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c over a group's slots c, slots in order, eight in flight.  LG =
+// head_dim / 4 lanes hold a query row (four elements each).  A group of few rows has many slots (one long request: 64):
+// there a block's waves take every fourth slot of the same rows and are joined in order.
+template <int HD>
 __global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restrict__ groups, KvAttnArgs ka) {
-  __shared__ float sacc[4][64][4], sml[4];
+  __shared__ float sacc[4][64][4], sml[4][64];
   const AttnArgs &a = ka.a;
   const AttnGroup gr = groups[blockIdx.y];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int nw = gr.nq <= kAttnQB / 4 ? 4 : 1;             // waves a row
-  const int qloc = nw == 4 ? blockIdx.x : blockIdx.x * 4 + wave, G = a.nq / a.nkv, hd = a.hd;
+  constexpr int LG = HD / 4, RW = 64 / LG;                 // lanes a row, rows a wave
+  const int G = a.nq / a.nkv, e0 = 4 * (lane & (LG - 1));
+  const int qloc = (nw == 4 ? blockIdx.x : blockIdx.x * 4 + wave) * RW + lane / LG;
   if (qloc >= gr.nq) return;
-  const bool on = 4 * lane < hd;
   const float *po = reinterpret_cast<const float *>(a.part_o);
   const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
   // a lane's share of the slots' maxima
   float mx = -INFINITY;
-  for (int c = lane; c < gr.n; c += 64) mx = fmaxf(mx, ml[(size_t)(gr.first_slot + c) * kAttnQB + qloc].x);
-  mx = wave_max(mx);
+  for (int c = lane & (LG - 1); c < gr.n; c += LG) mx = fmaxf(mx, ml[(size_t)(gr.first_slot + c) * kAttnQB + qloc].x);
+  if constexpr (LG == 64) {
+    mx = wave_max(mx);
+  } else {
+#pragma unroll
+    for (int o = 1; o < LG; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+  }
   constexpr int CH = 8;
   float L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
   for (int c0 = nw == 4 ? wave : 0; c0 < gr.n; c0 += nw * CH) {
@@ -892,7 +899,7 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restr
       const bool live = c0 + nw * c < gr.n;
       const size_t r = (size_t)(gr.first_slot + (live ? c0 + nw * c : 0)) * kAttnQB + qloc;
       p[c] = live ? ml[r] : make_float2(-INFINITY, 0.f);
-      v[c] = live && on ? *reinterpret_cast<const float4 *>(po + r * hd + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+      v[c] = live ? *reinterpret_cast<const float4 *>(po + r * HD + e0) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -905,11 +912,11 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restr
   if (nw == 4) {                                           // the whole block
 #pragma unroll
     for (int j = 0; j < 4; ++j) sacc[wave][lane][j] = acc[j];
-    if (lane == 0) sml[wave] = L;
+    sml[wave][lane] = L;
     __syncthreads();
     if (wave > 0) return;
     for (int w = 1; w < 4; ++w) {
-      L += sml[w];
+      L += sml[w][lane];
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[j] += sacc[w][lane][j];
     }
@@ -917,10 +924,9 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restr
   const int qrow = gr.q0 + qloc;
   const size_t orow = (size_t)gr.tok_off + qrow / G;
   const int qg = gr.kvh * G + qrow % G;
-  if (a.lse && lane == 0) a.lse[orow * a.nq + qg] = (mx + log2f(L)) * 0.6931471805599453f;
-  if (!on) return;
+  if (a.lse && e0 == 0) a.lse[orow * a.nq + qg] = (mx + log2f(L)) * 0.6931471805599453f;
   const float inv = 1.0f / L;
-  const size_t col = (size_t)qg * hd + 4 * lane;
+  const size_t col = (size_t)qg * HD + e0;
   bf16x4 r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) r[j] = (bf16)(acc[j] * inv);
@@ -929,7 +935,14 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const AttnGroup *__restr
 
 hipError_t launch_kv4_merge(const AttnGroup *groups, int n_groups, const KvAttnArgs &a, hipStream_t s) {
   if (n_groups <= 0) return hipSuccess;
-  hipLaunchKernelGGL(kv4_merge_kernel, dim3(kAttnQB / 4, n_groups), dim3(256), 0, s, groups, a);
+  const dim3 grid(kAttnQB / 4 * a.a.hd / 256, n_groups);
+  switch (a.a.hd) {
+    case 32: hipLaunchKernelGGL(kv4_merge_kernel<32>, grid, dim3(256), 0, s, groups, a); break;
+    case 64: hipLaunchKernelGGL(kv4_merge_kernel<64>, grid, dim3(256), 0, s, groups, a); break;
+    case 128: hipLaunchKernelGGL(kv4_merge_kernel<128>, grid, dim3(256), 0, s, groups, a); break;
+    case 256: hipLaunchKernelGGL(kv4_merge_kernel<256>, grid, dim3(256), 0, s, groups, a); break;
+    default: return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 
