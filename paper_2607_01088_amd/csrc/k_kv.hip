@@ -420,60 +420,4 @@ hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16_mode, hipStre
   return hipGetLastError();
 }
 
-// ------------------------------------------------------------------ attention weight of cached tokens
-// mass_j = sum over the KV head's query rows r of exp(q_r . k_j / sqrt(hd) - lse_r).  fp32 mode: a
-// block holds kMassRows keys, a wave one of them at a time; its lane groups take
-// every NG-th query row.
-template <int HD, bool FP4>
-__global__ void __launch_bounds__(256) kv_mass_rows_kernel(KvMassArgs a) {
-  constexpr int LG = HD / 16, NG = 64 / LG;
-  const MassItem it = a.items[blockIdx.x];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % LG, g = lane / LG;
-  const int G = a.nq / a.nkv, R = it.H * G;
-  const float *qkv = reinterpret_cast<const float *>(a.qkv);
-  const size_t codes = kv4_code_bytes(a.L, it.P, a.nkv, HD);
-  const float scale = 1.0f / sqrtf((float)HD);
-  for (int kk = wave; kk < it.nk; kk += 4) {
-    const int key = it.k0 + kk;
-    float kf[16];
-    load16_cache<HD, float, FP4>(it.pk, codes, ((size_t)a.layer * it.P + key) * a.nkv + it.kvh, c, kf);
-    float sum = 0.f;
-    for (int r0 = 0; r0 < R; r0 += NG) {
-      const int r = min(r0 + g, R - 1);
-      const size_t row = (size_t)it.tok_off + r / G;
-      const int qg = it.kvh * G + r % G;
-      float q[16];
-      load16(qkv + row * a.ldqkv + (size_t)qg * HD + c * 16, q);
-      float dot = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dot = fmaf(q[e], kf[e], dot);
-      dot = group_sum<LG>(dot) * scale;
-      if (r0 + g < R) sum += expf(dot - a.lse[row * a.nq + qg]);
-    }
-#pragma unroll
-    for (int o = LG; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
-    if (lane == 0) {
-      float *m = it.mass + ((size_t)a.layer * a.nkv + it.kvh) * it.P + key;
-      *m = a.accumulate ? *m + sum : sum;
-    }
-  }
-}
-
-template <int HD>
-static void launch_mass_rows(const KvMassArgs &a, hipStream_t s) {
-  if (a.fp4) hipLaunchKernelGGL((kv_mass_rows_kernel<HD, true>), dim3(a.n_items), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((kv_mass_rows_kernel<HD, false>), dim3(a.n_items), dim3(256), 0, s, a);
-}
-
-hipError_t launch_kv_mass_rows(const KvMassArgs &a, hipStream_t s) {
-  switch (a.hd) {
-    case 32: launch_mass_rows<32>(a, s); break;
-    case 64: launch_mass_rows<64>(a, s); break;
-    case 128: launch_mass_rows<128>(a, s); break;
-    case 256: launch_mass_rows<256>(a, s); break;
-    default: return hipErrorInvalidValue;
-  }
-  return hipGetLastError();
-}
-
 }  // namespace rosa

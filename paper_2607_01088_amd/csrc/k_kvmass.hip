@@ -1,4 +1,4 @@
-// Attention weight of cached tokens on the matrix cores (gfx950), bf16 mode, one layer:
+// Attention weight of cached tokens on the matrix cores (gfx950), one layer:
 //   mass_j = sum over the KV head's query rows r of exp(q_r . k_j / sqrt(hd) - lse_r).
 //
 // S = Q K^T in 32 x 32 tiles with a key to each lane: the sum over query rows is then a sum over a lane's
@@ -8,7 +8,8 @@
 // different tiles of queries; each key's sum is made by one block in a fixed order (no atomics).
 // 256 requests of 512 to 1280 cached tokens, 16 or 50 action tokens x 8 heads, head_dim 256: 54 us over
 // a bf16 cache (a key at a time on the vector units: 2220), 45 us over a 4-bit one; one request's 816
-// tokens under 50: 9 (385).  Bounds: the products take 14 us of the matrix cores, K 24 us (bf16) of HBM.
+// tokens under 50: 9 (385).  In the fp32 mode the products are fp32 ones, a key tile fills the registers:
+// F40 us over 40 requests of 512 to 768 tokens (F40B), F1 over the one of 816 (F1B).  Bounds: the products take 14 us of the matrix cores, K 24 us (bf16) of HBM.
 #include <math.h>
 
 #include <type_traits>
@@ -29,17 +30,28 @@ __device__ __forceinline__ void dma_256(const float *base, uint32_t off, uint32_
 #pragma clang diagnostic pop
 }
 
-// A lane's half of a cached row (HD / 2 elements) in bf16, in the order of its operands: bf16 cache, operand i: 8
-// elements from 16 i + 8 half on; 4-bit cache: 8 from HD / 2 half + 8 i on (whole blocks, or half of one).
-template <int HD>
-__device__ __forceinline__ void read_key(const KvMassArgs &a, const MassItem &it, int key, int half, bool fp4, bf16x8 (&k)[HD / 16]) {
-  const size_t row = ((size_t)a.layer * it.P + key) * a.nkv + it.kvh;
-  if (!fp4) {
-    const bf16 *p = reinterpret_cast<const bf16 *>(it.pk) + row * HD + half * 8;
+// 16 bytes of a row, an operand: 8 bf16 or (four products of 2 elements each) 4 fp32
+template <typename T> struct MassOperand { typedef bf16x8 type; };
+template <> struct MassOperand<float> { typedef f32x4 type; };
+__device__ __forceinline__ f32x16 mass_product(bf16x8 q, bf16x8 k, f32x16 s) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, k, s, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mass_product(f32x4 q, f32x4 k, f32x16 s) {
 #pragma unroll
-    for (int i = 0; i < HD / 16; ++i) k[i] = *reinterpret_cast<const bf16x8 *>(p + 16 * i);
+  for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(q[e], k[e], s, 0, 0, 0);
+  return s;
+}
+
+// A lane's half of a cached row (HD / 2 elements) in the model's type, in the order of its operands: operand i is the
+// row's chunk of 16 bytes 2 i + half, of a 4-bit cache the chunk i of the row's half (whole blocks, or half of one).
+template <int HD, typename T, bool FP4>
+__device__ __forceinline__ void read_key(const KvMassArgs &a, const MassItem &it, int key, int half,
+                                         typename MassOperand<T>::type (&k)[HD * (int)sizeof(T) / 32]) {
+  const size_t row = ((size_t)a.layer * it.P + key) * a.nkv + it.kvh;
+  if constexpr (!FP4) {
+    const uint8_t *p = reinterpret_cast<const uint8_t *>(it.pk) + row * HD * sizeof(T) + half * 16;
+#pragma unroll
+    for (int i = 0; i < HD * (int)sizeof(T) / 32; ++i) k[i] = *reinterpret_cast<const typename MassOperand<T>::type *>(p + 32 * i);
     return;
-  }
+  } else {
   constexpr int NW = HD / 16, NB = HD >= 64 ? HD / 64 : 1;      // code words, blocks
   const uint8_t *p = reinterpret_cast<const uint8_t *>(it.pk) + row * (HD / 2) + half * (HD / 4);
   const uint8_t *sp = reinterpret_cast<const uint8_t *>(it.pk) + kv4_code_bytes(a.L, it.P, a.nkv, HD) + row * (HD / 32) +
@@ -59,12 +71,21 @@ __device__ __forceinline__ void read_key(const KvMassArgs &a, const MassItem &it
 #pragma unroll
   for (int j = 0; j < NB; ++j) s[j] = sp[j];
 #pragma unroll
-  for (int i = 0; i < NW; ++i) k[i] = kv4_bf16x8(w[i], kv4_scale(s[i / 4]));
+  for (int i = 0; i < NW; ++i) {
+    const bf16x8 v = kv4_bf16x8(w[i], kv4_scale(s[i / 4]));
+    if constexpr (sizeof(T) == 2) {
+      k[i] = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[2 * i + e / 4][e % 4] = (float)v[e];
+    }
+  }
+  }
 }
 
-template <int HD, int KT, int WK>
+template <int HD, typename T, int KT, int WK>
 struct MassTile {
-  static constexpr int ROWB = HD * 2, CPR = ROWB / 16, TILEB = 32 * ROWB, NF = HD / 16;
+  static constexpr int ROWB = HD * (int)sizeof(T), CPR = ROWB / 16, TILEB = 32 * ROWB, NF = CPR / 2;
   static constexpr int WR = 4 / WK, KEYS = 32 * KT * WK;
   static constexpr int STAGEB = WR * TILEB, UNITS = STAGEB / 1024;      // a stage of the ring: WR query tiles
   static constexpr int DEPTH = 65536 / STAGEB < 4 ? 65536 / STAGEB : 4;
@@ -73,9 +94,10 @@ struct MassTile {
   static_assert(DEPTH >= 2 && LDSB <= 81920, "two blocks a CU");
 };
 
-template <int HD, int KT, int WK, bool FP4>
+template <int HD, typename E, int KT, int WK, bool FP4>
 __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
-  using T = MassTile<HD, KT, WK>;
+  using T = MassTile<HD, E, KT, WK>;
+  typedef typename MassOperand<E>::type operand;
   constexpr int ROWB = T::ROWB, CPR = T::CPR, NF = T::NF, WR = T::WR, DEPTH = T::DEPTH;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDSB];
   // Neighbouring items read the same queries: blocks of one XCD (every eighth) take a run of items.
@@ -85,7 +107,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
   const int col = lane & 31, half = lane >> 5, kg = wave % WK, rg = wave / WK;
   const int G = a.nq / a.nkv, R = it.H * G, n = (R + 32 * WR - 1) / (32 * WR);
   const float rG = 1.0f / (float)G;
-  const bf16 *qkv = reinterpret_cast<const bf16 *>(a.qkv);
+  const E *qkv = reinterpret_cast<const E *>(a.qkv);
   const uint32_t lds0 = lds_u32(smem);
 
   // The queries of stage t (rows past the last: the last one), whole rows side by side, chunk c of row r at
@@ -98,7 +120,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
     head = x - tok * G;
   };
   auto unit_row = [&](int j) { return (wave + 4 * j) * (64 / CPR) + lane / CPR; };
-  auto unit_col = [&](int r) { return ((lane % CPR) ^ at::swz(r, CPR)) * 8; };
+  auto unit_col = [&](int r) { return ((lane % CPR) ^ at::swz(r, CPR)) * (16 / (int)sizeof(E)); };
   // Where G divides a stage its rows lie the same way in each: lane offsets made once.
   const bool even = (32 * WR) % G == 0;
   uint32_t qoff[NU], loff;
@@ -107,7 +129,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
 #pragma unroll
     for (int j = 0; j < NU; ++j) {
       row_of(unit_row(j), 0, 32 * WR, tok, head);
-      qoff[j] = (uint32_t)(tok * a.ldqkv + head * HD + unit_col(unit_row(j))) * 2;
+      qoff[j] = (uint32_t)(tok * a.ldqkv + head * HD + unit_col(unit_row(j))) * (uint32_t)sizeof(E);
     }
     row_of(rg * 32 + col, 0, 32 * WR, tok, head);
     loff = (uint32_t)(tok * a.nq + head) * 4;
@@ -115,7 +137,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
   auto fetch = [&](int t) {
     const int base = t * 32 * WR, tok0 = base / G;
     const uint32_t st = lds0 + (uint32_t)(t % DEPTH * T::STAGEB), lst = lds0 + (uint32_t)(T::LSE + (t % DEPTH * 4 + wave) * 256);
-    const bf16 *q = qkv + (size_t)(it.tok_off + tok0) * a.ldqkv + (size_t)it.kvh * G * HD;
+    const E *q = qkv + (size_t)(it.tok_off + tok0) * a.ldqkv + (size_t)it.kvh * G * HD;
     const float *l = a.lse + (size_t)(it.tok_off + tok0) * a.nq + it.kvh * G;
     if (even && base + 32 * WR <= R) {
 #pragma unroll
@@ -140,10 +162,10 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
     if (t < n) fetch(t);
 
   const bool active = kg * KT * 32 < it.nk;
-  bf16x8 k[KT][NF];
+  operand k[KT][NF];
   if (active)
 #pragma unroll
-    for (int x = 0; x < KT; ++x) read_key<HD>(a, it, it.k0 + min((kg * KT + x) * 32 + col, it.nk - 1), half, FP4, k[x]);
+    for (int x = 0; x < KT; ++x) read_key<HD, E, FP4>(a, it, it.k0 + min((kg * KT + x) * 32 + col, it.nk - 1), half, k[x]);
   __builtin_amdgcn_s_waitcnt(at::waitcnt_vm(0));      // the keys, here: no wait for them is left to the loop
 
   const float sl2 = 1.4426950408889634f / sqrtf((float)HD);
@@ -161,9 +183,9 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
                         (uint32_t)(((FP4 ? NF * half : half) ^ at::swz(col, CPR)) << 4);
     constexpr int RA = KT == 2 || NF < 6 ? (NF < 4 ? NF : 4) : 6;            // operands are read RA - 1 ahead
     auto qfrag = [&](int i) {
-      return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds_ptr(q0 ^ (uint32_t)(i << (FP4 ? 4 : 5))));
+      return *reinterpret_cast<const __attribute__((address_space(3))) operand *>(lds_ptr(q0 ^ (uint32_t)(i << (FP4 ? 4 : 5))));
     };
-    bf16x8 q[RA];
+    operand q[RA];
 #pragma unroll
     for (int i = 0; i < RA - 1; ++i) q[i] = qfrag(i);
     // register r: query row (r / 4) 8 + 4 half + r % 4 of the tile
@@ -176,7 +198,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
       if (i + RA - 1 < NF) q[(i + RA - 1) % RA] = qfrag(i + RA - 1);
       else if (i + RA - 1 - NF < 4) l[i + RA - 1 - NF] = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(lds_ptr(l0 + (i + RA - 1 - NF) * 32));
 #pragma unroll
-      for (int x = 0; x < KT; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[i % RA], k[x][i], s[x], 0, 0, 0);
+      for (int x = 0; x < KT; ++x) s[x] = mass_product(q[i % RA], k[x][i], s[x]);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -225,17 +247,19 @@ __global__ void __launch_bounds__(256, 2) kv_mass_kernel(KvMassArgs a) {
   }
 }
 
-template <int HD, int KT, int WK>
+template <int HD, typename E, int KT, int WK>
 static void launch_mass(const KvMassArgs &a, hipStream_t s) {
-  static_assert(MassTile<HD, KT, WK>::KEYS == kMassLarge || MassTile<HD, KT, WK>::KEYS == kMassSmall, "item sizes");
-  if (a.fp4) hipLaunchKernelGGL((kv_mass_kernel<HD, KT, WK, true>), dim3(a.n_items), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((kv_mass_kernel<HD, KT, WK, false>), dim3(a.n_items), dim3(256), 0, s, a);
+  if (a.fp4) hipLaunchKernelGGL((kv_mass_kernel<HD, E, KT, WK, true>), dim3(a.n_items), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_mass_kernel<HD, E, KT, WK, false>), dim3(a.n_items), dim3(256), 0, s, a);
 }
 
 template <int HD>
-static hipError_t launch_mass_keys(const KvMassArgs &a, hipStream_t s) {
-  if (a.keys == kMassLarge) launch_mass<HD, 2, 4>(a, s);
-  else if (a.keys == kMassSmall) launch_mass<HD, 1, 2>(a, s);
+static hipError_t launch_mass_keys(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
+  static_assert(MassTile<HD, bf16, 2, 4>::KEYS == kMassLarge && MassTile<HD, bf16, 1, 2>::KEYS == kMassSmall &&
+                    MassTile<HD, float, 1, 4>::KEYS == kMassFloat, "item sizes");
+  if (!bf16_mode && a.keys == kMassFloat) launch_mass<HD, float, 1, 4>(a, s);
+  else if (bf16_mode && a.keys == kMassLarge) launch_mass<HD, bf16, 2, 4>(a, s);
+  else if (bf16_mode && a.keys == kMassSmall) launch_mass<HD, bf16, 1, 2>(a, s);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
@@ -243,17 +267,16 @@ static hipError_t launch_mass_keys(const KvMassArgs &a, hipStream_t s) {
 // Keys a block takes.  Large blocks read the queries from LDS once for two tiles of keys and from memory once for 256
 // keys; but a set of fewer than one of them for each CU is done sooner in small ones.
 int kv_mass_keys(bool bf16_mode, int64_t large_blocks) {
-  return !bf16_mode ? kMassRows : large_blocks >= 256 ? kMassLarge : kMassSmall;
+  return !bf16_mode ? kMassFloat : large_blocks >= 256 ? kMassLarge : kMassSmall;
 }
 
 hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16_mode, hipStream_t s) {
   if (a.n_items <= 0) return hipSuccess;
-  if (!bf16_mode) return launch_kv_mass_rows(a, s);
   switch (a.hd) {
-    case 32: return launch_mass_keys<32>(a, s);
-    case 64: return launch_mass_keys<64>(a, s);
-    case 128: return launch_mass_keys<128>(a, s);
-    case 256: return launch_mass_keys<256>(a, s);
+    case 32: return launch_mass_keys<32>(a, bf16_mode, s);
+    case 64: return launch_mass_keys<64>(a, bf16_mode, s);
+    case 128: return launch_mass_keys<128>(a, bf16_mode, s);
+    case 256: return launch_mass_keys<256>(a, bf16_mode, s);
     default: return hipErrorInvalidValue;
   }
 }

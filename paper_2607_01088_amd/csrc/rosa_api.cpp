@@ -1011,7 +1011,7 @@ rosa_status rosa_batch_create(const rosa_model_config *cfg, const rosa_weights *
     // many idle first entries (n_blocks <= items + 7)
     b->max_list_ints = (size_t)cap->max_steps * (2 * (size_t)b->max_items + 8 * kMaxLanes * n_sets);
     b->off_mass = align(b->off_lists + b->max_list_ints * sizeof(AttnItem));
-    b->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassRows) + (size_t)cap->max_requests);
+    b->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassSmall) + (size_t)cap->max_requests);
     b->plan_bytes = align(b->off_mass + b->max_mass * sizeof(MassItem));
     b->d_plan = dalloc<uint8_t>(b, b->plan_bytes, e);
     if (e != hipSuccess) {

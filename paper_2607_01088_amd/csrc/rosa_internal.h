@@ -330,7 +330,7 @@ struct MassItem {
   int32_t pad[2];
 };
 static_assert(sizeof(MassItem) == 48, "MassItem is 48 bytes");
-constexpr int kMassRows = 32, kMassSmall = 64, kMassLarge = 256;   // keys an item: fp32 mode, bf16 mode
+constexpr int kMassFloat = 128, kMassSmall = 64, kMassLarge = 256;   // keys an item (at most): fp32 mode, bf16 mode
 // Keys an item of a call whose caches make large_blocks items of kMassLarge keys
 int kv_mass_keys(bool bf16, int64_t large_blocks);
 struct KvMassArgs {
@@ -343,6 +343,5 @@ struct KvMassArgs {
   bool fp4, accumulate;
 };
 hipError_t launch_kv_mass(const KvMassArgs &a, bool bf16, hipStream_t s);
-hipError_t launch_kv_mass_rows(const KvMassArgs &a, hipStream_t s);      // fp32 mode
 
 }  // namespace rosa

@@ -265,7 +265,7 @@ rosa_status rosa_kv_create(const rosa_model_config *cfg, const rosa_capacity *ca
     h->max_groups = (size_t)n_sets * kAttnMaxSlots;
     h->max_items = (size_t)n_sets * (kAttnMaxSlots + (size_t)blocks);
     h->max_lists = 2 * h->max_items + 8 * (size_t)n_sets;
-    h->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassRows) + (size_t)cap->max_requests);
+    h->max_mass = (size_t)D.nkv * ((size_t)(cap->max_prefix_tokens / kMassSmall) + (size_t)cap->max_requests);
     auto align = [](size_t v) { return (v + 255) / 256 * 256; };
     h->off_items = 0;
     h->off_groups = align(h->off_items + (h->bf16 ? 0 : h->max_items) * sizeof(AttnItem));
