@@ -325,96 +325,118 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// One wave per query row.  LG = HD / 16 lanes hold a key (16 elements each), so 64 / LG
-// keys are under way at once, each lane group with a softmax of its own (running
-// maximum, sum, weighted values) over every (64 / LG)-th key; the groups join at the
-// end.  Everything in fp32.
-template <int HD, typename T, bool FP4>
+// fp32 mode.  A block takes four query rows, its four waves different keys.  LG = HD / 16 lanes hold a key (16
+// elements each), so 64 / LG keys are under way at once in a wave, read once for the four rows; each lane group
+// has a softmax of its own for each (running maximum, sum, weighted values); the groups join at the end, then the
+// waves through LDS, in order.  Vector units and the latency of K and V bound it: 40 requests of 512 to 768
+// tokens under 16 or 50, 8 heads of 256: F40A us over 4-bit caches, F40M over fp32 ones; one token over 816: FT.
+template <int HD, bool FP4>
 __global__ void __launch_bounds__(256) kv_attention_rows_kernel(KvAttnArgs ka) {
-  constexpr int LG = HD / 16, NG = 64 / LG;
+  constexpr int LG = HD / 16, NG = 64 / LG, RW = 4;
+  __shared__ float so[4][RW][HD], sm[4][RW], sl[4][RW];
   const AttnArgs &a = ka.a;
   const AttnItem it = a.items[blockIdx.x];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int qloc = blockIdx.y * 4 + wave;
-  if (qloc >= it.nq) return;
-  const int G = a.nq / a.nkv;
-  const int qrow = it.q0 + qloc;
-  const size_t row = (size_t)it.tok_off + qrow / G;
-  const int qg = it.kvh * G + qrow % G;
-  const int c = lane % LG, g = lane / LG;
-  const T *qkv = reinterpret_cast<const T *>(a.qkv);
-  float q[16], acc[16];
-  load16(qkv + row * a.ldqkv + (size_t)qg * HD + c * 16, q);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q0 = blockIdx.y * RW;
+  if (q0 >= it.nq) return;
+  const int G = a.nq / a.nkv, c = lane % LG, g = lane / LG;
+  const float *qkv = reinterpret_cast<const float *>(a.qkv);
+  float q[RW][16], acc[RW][16] = {}, m[RW], l[RW];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  for (int r = 0; r < RW; ++r) {
+    const int qrow = it.q0 + min(q0 + r, it.nq - 1);
+    load16(qkv + ((size_t)it.tok_off + qrow / G) * a.ldqkv + (size_t)(it.kvh * G + qrow % G) * HD + c * 16, q[r]);
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+  }
   const size_t codes = kv4_code_bytes(ka.L, it.P, a.nkv, HD);
   const float scale = 1.0f / sqrtf((float)HD);
-  float m = -INFINITY, l = 0.f;
-  for (int k0 = it.kbeg; k0 < it.kend; k0 += NG) {
+  for (int k0 = it.kbeg + wave * NG; k0 < it.kend; k0 += 4 * NG) {
     const int key = k0 + g;
     const bool on = key < it.kend;
     const int kk = on ? key : it.kend - 1;
     float kf[16], vf[16];
     if (kk < it.P) {
       const size_t r = ((size_t)a.layer * it.P + kk) * a.nkv + it.kvh;
-      load16_cache<HD, T, FP4>(it.pk, codes, r, c, kf);
-      load16_cache<HD, T, FP4>(it.pv, codes, r, c, vf);
+      load16_cache<HD, float, FP4>(it.pk, codes, r, c, kf);
+      load16_cache<HD, float, FP4>(it.pv, codes, r, c, vf);
     } else {
-      const T *p = qkv + ((size_t)it.tok_off + kk - it.P) * a.ldqkv + (size_t)(a.nq + it.kvh) * HD + c * 16;
+      const float *p = qkv + ((size_t)it.tok_off + kk - it.P) * a.ldqkv + (size_t)(a.nq + it.kvh) * HD + c * 16;
       load16(p, kf);
       load16(p + (size_t)a.nkv * HD, vf);
     }
-    float dot = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dot = fmaf(q[e], kf[e], dot);
-    dot = group_sum<LG>(dot) * scale;
-    if (!on) continue;
-    const float mn = fmaxf(m, dot), al = expf(m - mn), p = expf(dot - mn);
-    l = l * al + p;
+    for (int r = 0; r < RW; ++r) {
+      float dot = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = acc[e] * al + p * vf[e];
-    m = mn;
+      for (int e = 0; e < 16; ++e) dot = fmaf(q[r][e], kf[e], dot);
+      dot = group_sum<LG>(dot) * scale;
+      if (!on || dot == -INFINITY) continue;                // a weight of 0
+      const float mn = fmaxf(m[r], dot), al = expf(m[r] - mn), p = expf(dot - mn);
+      l[r] = l[r] * al + p;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[r][e] = acc[r][e] * al + p * vf[e];
+      m[r] = mn;
+    }
   }
-  float mx = m;
 #pragma unroll
-  for (int o = LG; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-  const float w = l > 0.f || l != l ? expf(m - mx) : 0.f;   // a group without keys adds nothing
-  l *= w;
+  for (int r = 0; r < RW; ++r) {
+    float mx = m[r];
 #pragma unroll
-  for (int o = LG; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
-  const float inv = 1.0f / l;
-  T *out = reinterpret_cast<T *>(a.o);
-  const size_t col = (size_t)qg * HD + c * 16;
+    for (int o = LG; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    const bool any = l[r] > 0.f || l[r] != l[r];            // a group without keys adds nothing
+    const float w = any ? expf(m[r] - mx) : 0.f;
+    float ls = l[r] * w;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    float v = l == l && w == 0.f ? 0.f : acc[e] * w;
+    for (int o = LG; o < 64; o <<= 1) ls += __shfl_xor(ls, o, 64);
 #pragma unroll
-    for (int o = LG; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    // row-major, or kb32
-    if (g == 0) out[a.o_rows > 0 ? kb32_offset(a.o_rows, row, col + e) : row * a.ldo + col + e] = from_f32<T>(v * inv);
+    for (int e = 0; e < 16; ++e) {
+      float v = any ? acc[r][e] * w : 0.f;
+#pragma unroll
+      for (int o = LG; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+      if (g == 0) so[wave][r][c * 16 + e] = v;
+    }
+    if (lane == 0) { sm[wave][r] = mx; sl[wave][r] = ls; }
   }
-  if (a.lse && lane == 0) a.lse[row * a.nq + qg] = mx + logf(l);
+  __syncthreads();
+  // a wave a row
+  if (q0 + wave >= it.nq) return;
+  const int qrow = it.q0 + q0 + wave, qg = it.kvh * G + qrow % G;
+  const size_t row = (size_t)it.tok_off + qrow / G;
+  float mx = -INFINITY, f[4], L = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w][wave]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float x = sl[w][wave];
+    f[w] = x > 0.f || x != x ? expf(sm[w][wave] - mx) : 0.f;
+    L += x * f[w];
+  }
+  const float inv = 1.0f / L;
+  float *out = reinterpret_cast<float *>(a.o);
+  for (int e = lane; e < HD; e += 64) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v += so[w][wave][e] * f[w];
+    const size_t col = (size_t)qg * HD + e;
+    out[a.o_rows > 0 ? kb32_offset(a.o_rows, row, col) : row * a.ldo + col] = v * inv;   // row-major, or kb32
+  }
+  if (a.lse && lane == 0) a.lse[row * a.nq + qg] = mx + logf(L);
 }
 
 template <int HD>
-static void launch_rows(const KvAttnArgs &a, bool bf16_mode, dim3 grid, hipStream_t s) {
-  if (bf16_mode) {
-    if (a.fp4) hipLaunchKernelGGL((kv_attention_rows_kernel<HD, bf16, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((kv_attention_rows_kernel<HD, bf16, false>), grid, dim3(256), 0, s, a);
-  } else {
-    if (a.fp4) hipLaunchKernelGGL((kv_attention_rows_kernel<HD, float, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((kv_attention_rows_kernel<HD, float, false>), grid, dim3(256), 0, s, a);
-  }
+static void launch_rows(const KvAttnArgs &a, dim3 grid, hipStream_t s) {
+  if (a.fp4) hipLaunchKernelGGL((kv_attention_rows_kernel<HD, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_attention_rows_kernel<HD, false>), grid, dim3(256), 0, s, a);
 }
 
-hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16_mode, hipStream_t s) {
+hipError_t launch_kv_attention_rows(const KvAttnArgs &a, hipStream_t s) {
   if (a.a.n_items <= 0) return hipSuccess;
   dim3 grid(a.a.n_items, kAttnQB / 4);
   switch (a.a.hd) {
-    case 32: launch_rows<32>(a, bf16_mode, grid, s); break;
-    case 64: launch_rows<64>(a, bf16_mode, grid, s); break;
-    case 128: launch_rows<128>(a, bf16_mode, grid, s); break;
-    case 256: launch_rows<256>(a, bf16_mode, grid, s); break;
+    case 32: launch_rows<32>(a, grid, s); break;
+    case 64: launch_rows<64>(a, grid, s); break;
+    case 128: launch_rows<128>(a, grid, s); break;
+    case 256: launch_rows<256>(a, grid, s); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

@@ -947,7 +947,7 @@ hipError_t launch_kv4_merge(const AttnGroup *groups, int n_groups, const KvAttnA
 }
 
 hipError_t launch_kv_attention(const KvAttnArgs &ka, const AttnGroup *groups, int n_groups, bool bf16_mode, hipStream_t s) {
-  if (!bf16_mode) return launch_kv_attention_rows(ka, false, s);
+  if (!bf16_mode) return launch_kv_attention_rows(ka, s);
   const AttnArgs &a = ka.a;
   if (ka.fp4) {
     const hipError_t e = launch_kv4_attention(ka, s);

@@ -310,9 +310,8 @@ struct KvAttnArgs {
   int L;                 // layers of the caches
   bool fp4;
 };
-// One wave per query row, fp32 throughout (`bf16`: the type of qkv, o and model-type
-// caches): the fp32 mode's kernel.  Items are not split over keys.
-hipError_t launch_kv_attention_rows(const KvAttnArgs &a, bool bf16, hipStream_t s);
+// The fp32 mode's kernel.  Items are not split over keys.
+hipError_t launch_kv_attention_rows(const KvAttnArgs &a, hipStream_t s);
 // bf16 mode, 4-bit caches: the launch lists of a (ordered, n_blocks); partial results
 // of split items as part_o [slot][kAttnQB][hd] fp32 and part_ml.
 hipError_t launch_kv4_attention(const KvAttnArgs &a, hipStream_t s);
