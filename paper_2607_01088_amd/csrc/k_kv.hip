@@ -19,7 +19,8 @@ namespace rosa {
 // data the least error (relative 0.1119; 6: 0.1154, 8: 0.1150).
 //
 // A thread takes 8 elements (16 or 32 bytes in, 4 bytes of codes out, both
-// contiguous over a wave), four threads a block.
+// contiguous over a wave), four threads a block.  One pass, memory bound: 32 bf16 caches of 512 to 1280
+// tokens (644 MB each way) take 137 us, and 131 back: 4.7 and 4.9 TB/s where a copy reaches 5.0.
 template <typename T>
 __global__ void __launch_bounds__(256) kv_quantize_kernel(KvJobs jobs, int L, int nkv, int hd) {
   const KvJob &j = jobs.j[blockIdx.y];
@@ -226,7 +227,8 @@ __global__ void __launch_bounds__(1024) kv_select_kernel(KvEvictJobs jobs, int r
   }
 }
 
-// The kept tokens' rows (K and V): 16-byte pieces, `pieces` of them a row.  Rows of the
+// The kept tokens' rows (K and V): 16-byte pieces, `pieces` of them a row; at the copy's rate (half of 32 caches,
+// 513 MB read and written: 93 us).  Rows of the
 // caches are [L][tokens][nkv]; destination row r = (layer keep + i) nkv + head.
 __global__ void __launch_bounds__(256) kv_gather_kernel(KvEvictJobs jobs, int L, int nkv, int pieces) {
   const KvEvictJob &j = jobs.j[blockIdx.y];
@@ -329,7 +331,8 @@ __device__ __forceinline__ float group_sum(float v) {
 // elements each), so 64 / LG keys are under way at once in a wave, read once for the four rows; each lane group
 // has a softmax of its own for each (running maximum, sum, weighted values); the groups join at the end, then the
 // waves through LDS, in order.  Vector units and the latency of K and V bound it: 40 requests of 512 to 768
-// tokens under 16 or 50, 8 heads of 256: F40A us over 4-bit caches, F40M over fp32 ones; one token over 816: FT.
+// tokens under 16 or 50, 8 heads of 256: 450 us over caches of either format (860 over fp32 ones with a wave a row and
+// no key shared); one token over 816: 87.
 template <int HD, bool FP4>
 __global__ void __launch_bounds__(256) kv_attention_rows_kernel(KvAttnArgs ka) {
   constexpr int LG = HD / 16, NG = 64 / LG, RW = 4;
