@@ -135,6 +135,7 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
  *   o:   DEVICE [sum H][n_q head_dim], model dtype, written
  *   lse: DEVICE [sum H][n_q] fp32, written: ln sum_j exp(q.k_j / sqrt(head_dim))
  *        over all keys the row attends to; may be NULL
+ * o and lse may not overlap each other or what the call reads.
  * In the bf16 mode the softmax weights are rounded to bf16 for the product with the
  * values; statistics and sums are fp32.  Errors: ROSA_E_INVALID (no plan,
  * NULL or misaligned pointers, layer out of range), ROSA_E_DEVICE. */

@@ -34,6 +34,7 @@ struct rosa_kv {
     int groups = 0, group_base = 0;
   } sets[2];
   int n_mass = 0, mass_keys = 0;
+  size_t rows = 0;                   // of the planned set
 
   // device plan region, two pinned staging copies
   uint8_t *d_plan = nullptr;
@@ -387,6 +388,7 @@ rosa_status rosa_kv_plan(rosa_kv *h, const rosa_request *reqs, int32_t n, int32_
     h->n = n;
     h->n_mass = (int)mi.size();
     h->mass_keys = keys;
+    h->rows = (size_t)p.M0;
     h->has_mass = mass != nullptr;
     h->fp4 = format == ROSA_KV_FP4;
     h->planned = true;
@@ -409,6 +411,12 @@ rosa_status rosa_kv_attention(rosa_kv *h, int32_t layer, const void *qkv, void *
     if (h->n == 0) return ROSA_OK;
     if (!qkv || !o || !aligned(qkv, 16) || !aligned(o, 16) || !aligned(lse, 4))
       return fail(h, ROSA_E_INVALID, "qkv or o is NULL, or an array is misaligned");
+    const size_t es = h->bf16 ? 2 : 4;
+    std::vector<Range> ranges;
+    add_range(ranges, qkv, h->rows * D.qkv_dim * es, false);
+    add_range(ranges, o, h->rows * D.o_dim * es, true);
+    add_range(ranges, lse, h->rows * D.nq * 4, true);
+    if (clash(ranges)) return fail(h, ROSA_E_INVALID, "o or lse overlaps another array of the call");
     DeviceGuard guard(h->device);
     hipError_t e = guard.error();
     const rosa_kv::Set &S = h->sets[attn_set_of(&h->cfg, layer)];

@@ -112,6 +112,27 @@ def test_masses_of_two_requests_may_not_share_memory():
     h.close()
 
 
+def test_outputs_that_overlap_are_refused():
+    from paper_2607_01088_amd import rosa
+    b = Batch(HD64_SHAPE, "bf16", 1, [(64, 3), (10, 2)], seed=5)
+    h = rosa.KvAttention(b.shape, b.dtype, b.cap)
+    h.plan(b.structs, 1)
+    qkv, o, lse = b.qkv, b.o.all, b.lse.all
+    n = b.qkv.numel() * 2
+    room = torch.empty(2 * n + 4096, dtype=torch.uint8, device="cuda")
+    room[:n] = qkv.view(torch.uint8).flatten()
+    for bad in ((qkv, qkv, lse), (qkv, o, qkv), (qkv, o, o), (room[:n], room[n - 16:], lse)):
+        with pytest.raises(rosa.RosaError) as e:
+            h.attention(0, bad[0], bad[1], lse=bad[2])
+        assert e.value.status == rosa.ROSA_E_INVALID
+    h.attention(0, room[:n], room[n:], lse=lse)                          # side by side
+    h.attention(0, qkv, o, lse=None)
+    torch.cuda.synchronize()
+    check_batch(b, 0, b.out()[0], None)
+    assert torch.equal(room[n:n + b.o.n], b.o.data)
+    h.close()
+
+
 @pytest.mark.parametrize("fmt", [0, 1], ids=["model", "fp4"])
 def test_eviction_from_long_rows(fmt):
     specs = [(12287, 5000, 4, 48), (12288, 1, 0, 0), (12289, 12288, 0, 0), (20001, 15000, 4, 48), (40000, 100, 0, 3), (4096, 17, 1, 1),
