@@ -87,7 +87,7 @@ __device__ __forceinline__ void prefetch_weights(const WeightPrefetch (&pf)[kPre
 // max(causal_b, t + 1) in the tiles that reach it.
 // LSE: the rows' log-sum-exp goes to a.lse; the softmax sums are then taken in fp32
 // before the weights are rounded to bf16 (sums of rounded weights would leave a
-// log-sum-exp of bf16's accuracy).
+// log-sum-exp of bf16's accuracy), and split items leave their parts in fp32.
 template <int HD, int NG, bool CAUSAL, bool LSE>
 __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
   using at::TK;
@@ -499,6 +499,21 @@ __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
     const float l_all = l_run[g] + __shfl_xor(l_run[g], 32, 64);
     const int loc = 32 * (wave + 4 * g) + (lane & 31);
     if (loc >= it.nq) continue;
+    if constexpr (LSE) {
+      // A split item's O leaves in fp32, as the 4-bit caches' does: parts in bf16 would be a third rounding.
+      if (it.slot >= 0) {
+        float *po = reinterpret_cast<float *>(a.part_o) + ((size_t)it.slot * kAttnQB + loc) * HD + 4 * half;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int rg = 0; rg < 4; ++rg)
+            *reinterpret_cast<float4 *>(po + 32 * n + 8 * rg) =
+                make_float4(o[g][n][rg * 4], o[g][n][rg * 4 + 1], o[g][n][rg * 4 + 2], o[g][n][rg * 4 + 3]);
+        if (half == 0)
+          *reinterpret_cast<float2 *>(a.part_ml + ((size_t)it.slot * kAttnQB + loc) * 2) = make_float2(m_ref[g] * sl2, l_all);
+        continue;
+      }
+    }
     // Through LDS (the rings, free now): lane q writes its query row's 8-byte
     // pieces, chunk c of a row at c ^ (q % CPRO); then rows go out as whole
     // 16-byte chunks, consecutive lanes on consecutive chunks of a row.  A
@@ -523,7 +538,7 @@ __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
     }
     if constexpr (LSE) {
       const int qrow = it.q0 + loc;
-      if (it.slot < 0 && half == 0)
+      if (half == 0)
         a.lse[(size_t)(it.tok_off + qrow / G) * a.nq + it.kvh * G + qrow % G] = (m_ref[g] * sl2 + log2f(l_all)) * 0.6931471805599453f;
     }
   }
@@ -531,7 +546,7 @@ __global__ void __launch_bounds__(256, 2) attention_bf16_kernel(AttnArgs a) {
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const int base = 32 * (wave + 4 * g);
-    if (base >= it.nq) continue;
+    if (base >= it.nq || (LSE && it.slot >= 0)) continue;
     const uint8_t *stg = smem + (wave * NG + g) * (32 * 2 * HD);
     constexpr int RPI = 64 / CPRO;          // rows per instruction
 #pragma unroll
@@ -624,8 +639,7 @@ template <typename OutT>
 __global__ void __launch_bounds__(256) attn_merge_kernel(const AttnGroup *__restrict__ groups,
                                                          const bf16 *__restrict__ part_o,
                                                          const float *__restrict__ part_ml, OutT *o,
-                                                         int ldo, int nq, int nkv, int hd, int o_rows,
-                                                         float *lse) {
+                                                         int ldo, int nq, int nkv, int hd, int o_rows) {
   const AttnGroup gr = groups[blockIdx.y];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int qloc = blockIdx.x * 4 + wave;
@@ -672,7 +686,6 @@ __global__ void __launch_bounds__(256) attn_merge_kernel(const AttnGroup *__rest
     }
     mx = nm;
   }
-  if (lse && lane == 0) lse[(size_t)(tok_off + qt) * nq + qg] = (mx + log2f(L)) * 0.6931471805599453f;
   if (!on) return;
   const float inv = 1.0f / L;
   const size_t orow = (size_t)(tok_off + qt), col = (size_t)qg * hd + e0;
@@ -719,17 +732,17 @@ hipError_t launch_attention(const AttnArgs &a, bool bf16_mode, hipStream_t s) {
 }
 
 hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const void *part_o, const float *part_ml, void *o, int ldo, int nq,
-                             int nkv, int hd, bool bf16_mode, hipStream_t s, int o_rows, float *lse) {
+                             int nkv, int hd, bool bf16_mode, hipStream_t s, int o_rows) {
   if (n_groups <= 0) return hipSuccess;
   if (hd > 256) return hipErrorInvalidValue;   // a lane holds at most 4 head-dim elements
   if (o_rows > 0 && !bf16_mode) return hipErrorInvalidValue;
   dim3 grid(kAttnQB / 4, n_groups);
   if (bf16_mode)
     hipLaunchKernelGGL(attn_merge_kernel<bf16>, grid, dim3(256), 0, s, groups, (const bf16 *)part_o, part_ml,
-                       (bf16 *)o, ldo, nq, nkv, hd, o_rows, lse);
+                       (bf16 *)o, ldo, nq, nkv, hd, o_rows);
   else
     hipLaunchKernelGGL(attn_merge_kernel<float>, grid, dim3(256), 0, s, groups, (const bf16 *)part_o, part_ml,
-                       (float *)o, ldo, nq, nkv, hd, 0, lse);
+                       (float *)o, ldo, nq, nkv, hd, 0);
   return hipGetLastError();
 }
 

@@ -954,9 +954,10 @@ hipError_t launch_kv_attention(const KvAttnArgs &ka, const AttnGroup *groups, in
     return e != hipSuccess ? e : launch_kv4_merge(groups, n_groups, ka, s);
   }
   const hipError_t e = launch_attention(a, true, s);
-  return e != hipSuccess ? e
-                         : launch_attn_merge(groups, n_groups, a.part_o, a.part_ml, a.o, a.ldo, a.nq, a.nkv, a.hd, true, s,
-                                             a.o_rows, a.lse);
+  if (e != hipSuccess) return e;
+  // with the log-sum-exp split items leave their parts in fp32
+  return a.lse ? launch_kv4_merge(groups, n_groups, ka, s)
+               : launch_attn_merge(groups, n_groups, a.part_o, a.part_ml, a.o, a.ldo, a.nq, a.nkv, a.hd, true, s, a.o_rows);
 }
 
 }  // namespace rosa

@@ -233,7 +233,7 @@ struct AttnArgs {
   void *o; int ldo;                // o at column g*hd
   int o_rows;                      // bf16: 0 row-major (ldo), else kb32 planes of o_rows rows
   int nq, nkv, hd;
-  void *part_o;                    // [slot][kAttnQB][hd] bf16 (unnormalised O of split items)
+  void *part_o;                    // [slot][kAttnQB][hd] bf16, with lse fp32 (unnormalised O of split items)
   float *part_ml;                  // [slot][kAttnQB][2] fp32 (running max in log2 units, sum)
   // bf16: n_prefetch more blocks (a multiple of 8, after the n_blocks) read the
   // prefetch matrices and nothing else: block b, on XCD b % 8, its XCD's eighth of every
@@ -272,7 +272,7 @@ inline hipError_t upload_gemm_weights(void *dst, const float *src, int L, int K,
 void attn_order_items(const std::vector<AttnItem> &items, const int32_t *order, const int32_t *next, size_t n,
                       AttnItem *dst);
 hipError_t launch_attn_merge(const AttnGroup *groups, int n_groups, const void *part_o, const float *part_ml, void *o, int ldo, int nq,
-                             int nkv, int hd, bool bf16, hipStream_t s, int o_rows = 0, float *lse = nullptr);
+                             int nkv, int hd, bool bf16, hipStream_t s, int o_rows = 0);
 
 // ------------------------------------------------------------------ 4-bit caches and eviction
 // One 4-bit cache (K or V of one request): codes [L][P][nkv][hd / 2] bytes, then
